@@ -331,6 +331,87 @@ typedef struct {
 size_t s4c_verify_step_workspace_size(const s4c_attn_shape* shape, int32_t V);
 s4c_status s4c_verify_step(const s4c_step* step, void* hip_stream);
 
+/* ---- Changed scores, and a cache that rows are evicted from --------------------------------------------------------------
+ * A long conversation outgrows any cache.  s4c_kv_weigh adds up how much attention every cache row gets, s4c_kv_evict cuts the
+ * cache down to the rows that got most and the most recent ones, and s4c_tree_attn_scored attends to what is left, for models
+ * that cap their scores or bias them by distance too.  Rows of an evicted cache lie in no particular order, so each has its position:
+ *
+ *   s4c_tree_attn_scored -> s4c_accept_path -> s4c_kv_compact -> s4c_kv_weigh -> (root_pos += accept_len + 1) -> now and then s4c_kv_evict
+ */
+typedef struct {
+    float cap;                /* > 0: a score x = scale q.k becomes cap * tanh(x / cap); 0: it stays.  2 cap log2(e) and scale / cap
+                                 must be finite in fp32 */
+    const float* slopes;      /* [Hq] nullable: slopes[h] * (position of the key - position of the root) is added to it (a penalty on
+                                 distance has slopes > 0).  For a node of depth d this differs from the distance to the node by
+                                 slopes[h] * d on every key, which changes lse and not the output */
+    int32_t* key_pos;         /* [B][Hkv][S_cap] nullable: position of every cache row.  NULL: row j has position j, and the root
+                                 the position of the row that it is appended to.  Read only where slopes are given; s4c_kv_weigh
+                                 writes those of the path's rows */
+    const int32_t* root_pos;  /* [B] position of node 0, required with key_pos; a node of depth d has root_pos + d */
+} s4c_score;
+
+/* s4c_tree_attn with changed scores.  Everything not named here is as in s4c_tree_attn (workspace size, status, limits).
+ *   score  host pointer, nullable (nothing changed)
+ *   lse    [B][N][Hq] fp32 nullable: natural log of the sum of exp(changed score) over the keys that the row sees; +infinity for
+ *          the rows of a flagged sequence.  The biggest error is that of the scores, which are fp32.
+ * Results are deterministic; with no cap and no slopes `out` is s4c_tree_attn's up to rounding of the scores. */
+s4c_status s4c_tree_attn_scored(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree,
+                                const void* v_tree, const void* k_cache, const void* v_cache, const int32_t* cache_len,
+                                const int32_t* parent, int32_t max_cache_len, float scale, void* out, float* lse, int32_t* status,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+/* ... over a paged cache (layout and flagging as in s4c_tree_attn_paged; key_pos is by logical row, [B][Hkv][max_blocks * page_size]) */
+s4c_status s4c_tree_attn_scored_paged(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree,
+                                      const void* v_tree, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                                      int32_t max_blocks, int32_t page_size, int32_t num_pages, const int32_t* cache_len,
+                                      const int32_t* parent, int32_t max_cache_len, float scale, void* out, float* lse,
+                                      int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The attention weight that the accepted path's rows gave to every cache row, added to the rows' totals.  Called for each layer,
+ * after the path's rows were appended (s4c_kv_compact / s4c_commit_path), with the layer's q and lse:
+ *   weight[b][g][j] = (j < first ? weight_in[b][g][j] : 0) + sum over k, and over the heads h of KV head g, of exp(x - lse[b][path[k]][h])
+ *   for j < cache_len[b], where first = cache_len[b] - (accept_len[b] + 1), x the changed score of path node k's query (head h) and cache row
+ *   j, and only k = 0 .. accept_len[b] with j <= first + k count (a node sees the cache and its ancestors).
+ *   q          [B][N][Hq][D]          k_cache [B][Hkv][S_cap][D]          lse [B][N][Hq] of s4c_tree_attn_scored
+ *   cache_len  [B] with the path's rows, 1 .. min(max_cache_len, S_cap)     path [B][max_path], accept_len [B] as s4c_accept_path left them
+ *   score, scale  as the attention had them, but that key_pos, if given, also RECEIVES the positions of the path's rows (row first + k:
+ *              root_pos + k); root_pos is the root's of that attention call
+ *   weight_in, weight  [B][Hkv][S_cap] fp32, the same array or two that do not overlap; rows from cache_len[b] on are not written
+ *   status     [B] nullable: S4C_SEQ_BAD_LEN if cache_len, accept_len, the path or a page is not valid; nothing of that sequence is written.
+ * Sums are fp32 in a fixed order: results are deterministic. */
+s4c_status s4c_kv_weigh(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_cache, const float* lse,
+                        const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path,
+                        int32_t max_cache_len, float scale, const float* weight_in, float* weight, int32_t* status, void* hip_stream);
+s4c_status s4c_kv_weigh_paged(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_pool,
+                              const int32_t* block_table, int32_t max_blocks, int32_t page_size, int32_t num_pages, const float* lse,
+                              const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path,
+                              int32_t max_cache_len, float scale, const float* weight_in, float* weight, int32_t* status,
+                              void* hip_stream);
+
+/* Cuts every (layer, sequence, KV head) that has more than `budget` rows down to `budget`: rows whose position is at least next_pos[b] -
+ * recent come first, then those of the largest totals, equal ones by the lowest row.  Rows that stay below `budget` keep their place;
+ * those from `budget` on move, in row order, into the places of the evicted ones, in row order.
+ *   k_cache, v_cache  [layers][B][Hkv][S_cap][D], in place          cache_len [B] of all layers, 0 .. S_cap
+ *   weight_in, key_pos_in, weight, key_pos  [layers][B][Hkv][S_cap] before and after, each the same array or two that do not overlap;
+ *                rows below the new length are written.  Totals must not be NaN
+ *   next_pos [B] position of the next token            1 <= budget, 0 <= recent <= budget
+ *   new_len  [B] the length after, min(cache_len, budget) (may be cache_len itself)
+ *   kept     [layers][B][Hkv][budget] nullable: the row that row i was before, -1 behind the new length
+ *   status   [B] nullable: S4C_SEQ_BAD_LEN if cache_len or a page is not valid; then only new_len (unchanged) and kept (-1) are written.
+ *   workspace >= s4c_kv_evict_workspace_size(...) bytes, 256-byte aligned, contents need not be initialised
+ * Only B, Hkv, D, S_cap and dtype of `shape` are used.  Cache rows from the new length on are left as they were. */
+size_t s4c_kv_evict_workspace_size(int32_t layers, int32_t B, int32_t Hkv, int32_t budget, int32_t S_cap);
+s4c_status s4c_kv_evict(const s4c_attn_shape* shape, int32_t layers, void* k_cache, void* v_cache, const float* weight_in,
+                        const int32_t* key_pos_in, const int32_t* cache_len, const int32_t* next_pos, int32_t budget, int32_t recent,
+                        float* weight, int32_t* key_pos, int32_t* new_len, int32_t* kept, int32_t* status, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+/* ... of paged pools [layers][num_pages][Hkv][page_size][D] behind one block table (as in s4c_commit_path_paged): shape->S_cap =
+ * max_blocks * page_size, totals and positions by logical row.  Pages that hold no row below the new length are free afterwards. */
+s4c_status s4c_kv_evict_paged(const s4c_attn_shape* shape, int32_t layers, void* k_pool, void* v_pool, const int32_t* block_table,
+                              int32_t max_blocks, int32_t page_size, int32_t num_pages, const float* weight_in,
+                              const int32_t* key_pos_in, const int32_t* cache_len, const int32_t* next_pos, int32_t budget,
+                              int32_t recent, float* weight, int32_t* key_pos, int32_t* new_len, int32_t* kept, int32_t* status,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Text for a status code (any integer: unknown codes get "unknown status").  Static, never NULL. */
 const char* s4c_strerror(int code);
 

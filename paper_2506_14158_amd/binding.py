@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -25,7 +25,8 @@ EXPORTS = ("s4c_tree_attn_workspace_size", "s4c_tree_attn", "s4c_accept_path_wor
            "s4c_accept_path", "s4c_kv_compact", "s4c_strerror", "s4c_tree_attn_num_splits",
            "s4c_accept_resample", "s4c_accept_resample_workspace_size", "s4c_commit_path", "s4c_build_tree", "s4c_build_tree_workspace_size",
            "s4c_draft_linear", "s4c_draft_linear_workspace_size", "s4c_tree_attn_paged", "s4c_kv_compact_paged", "s4c_commit_path_paged", "s4c_accept_path_static",
-           "s4c_verify_step", "s4c_verify_step_workspace_size")
+           "s4c_verify_step", "s4c_verify_step_workspace_size", "s4c_tree_attn_scored", "s4c_tree_attn_scored_paged", "s4c_kv_weigh",
+           "s4c_kv_weigh_paged", "s4c_kv_evict", "s4c_kv_evict_paged", "s4c_kv_evict_workspace_size")
 
 
 class S4CError(RuntimeError):
@@ -37,6 +38,21 @@ class S4CError(RuntimeError):
 class AttnShape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "D", "N", "S_cap", "dtype")]
 
+
+class _Score(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("key_pos", C.c_void_p), ("root_pos", C.c_void_p)]
+
+
+class Score(NamedTuple):
+    """How attention scores are changed (s4c_score): x becomes cap * tanh(x / cap) where cap > 0; slopes [Hq] (fp32) times the key's position
+    from the root's is added; key_pos [B][Hkv][S_cap] and root_pos [B] (int32) where rows do not lie in order."""
+    cap: float = 0.0
+    slopes: Optional[torch.Tensor] = None
+    key_pos: Optional[torch.Tensor] = None
+    root_pos: Optional[torch.Tensor] = None
+
+
+PLAIN_SCORE = Score()
 
 _lib = None
 
@@ -95,6 +111,26 @@ def lib() -> C.CDLL:
             C.c_void_p] * 6
         L.s4c_verify_step_workspace_size.restype = C.c_size_t
         L.s4c_verify_step_workspace_size.argtypes = [C.POINTER(AttnShape), C.c_int32]
+        L.s4c_tree_attn_scored.restype = C.c_int
+        L.s4c_tree_attn_scored.argtypes = [C.POINTER(AttnShape), C.POINTER(_Score)] + [C.c_void_p] * 7 + [
+            C.c_int32, C.c_float] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        L.s4c_tree_attn_scored_paged.restype = C.c_int
+        L.s4c_tree_attn_scored_paged.argtypes = [C.POINTER(AttnShape), C.POINTER(_Score)] + [C.c_void_p] * 6 + [C.c_int32] * 3 + [
+            C.c_void_p] * 2 + [C.c_int32, C.c_float] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        L.s4c_kv_weigh.restype = C.c_int
+        L.s4c_kv_weigh.argtypes = [C.POINTER(AttnShape), C.POINTER(_Score)] + [C.c_void_p] * 6 + [C.c_int32] * 2 + [C.c_float] + [
+            C.c_void_p] * 4
+        L.s4c_kv_weigh_paged.restype = C.c_int
+        L.s4c_kv_weigh_paged.argtypes = [C.POINTER(AttnShape), C.POINTER(_Score)] + [C.c_void_p] * 3 + [C.c_int32] * 3 + [
+            C.c_void_p] * 4 + [C.c_int32] * 2 + [C.c_float] + [C.c_void_p] * 4
+        L.s4c_kv_evict_workspace_size.restype = C.c_size_t
+        L.s4c_kv_evict_workspace_size.argtypes = [C.c_int32] * 5
+        L.s4c_kv_evict.restype = C.c_int
+        L.s4c_kv_evict.argtypes = [C.POINTER(AttnShape), C.c_int32] + [C.c_void_p] * 6 + [C.c_int32] * 2 + [C.c_void_p] * 6 + [
+            C.c_size_t, C.c_void_p]
+        L.s4c_kv_evict_paged.restype = C.c_int
+        L.s4c_kv_evict_paged.argtypes = [C.POINTER(AttnShape), C.c_int32] + [C.c_void_p] * 3 + [C.c_int32] * 3 + [C.c_void_p] * 4 + [
+            C.c_int32] * 2 + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         L.s4c_strerror.restype = C.c_char_p
         L.s4c_strerror.argtypes = [C.c_int]
         _lib = L
@@ -460,6 +496,182 @@ def s4c_draft_linear(e, f, W, out, bias=None, workspace: Optional[torch.Tensor] 
     _check(lib().s4c_draft_linear(T, H, Hout, _dtype_code(e), _ptr(e), _ptr(f), _ptr(W), _ptr(bias), _ptr(out),
                                   _ptr(workspace), ws_bytes, _stream()))
     return out
+
+
+# ---- changed scores, and a cache that rows are evicted from
+def _need(t, dtype, shape, what):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise TypeError("%s must be %s %s, got %s %s" % (what, dtype, list(shape), t.dtype, list(t.shape)))
+
+
+def _one_device(*tensors):
+    """The call goes to the current device's stream: its tensors have to be there."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError("libs4c takes device tensors of the current device (cuda:%d), got %s" % (here, t.device))
+
+
+def _score(score, B, Hq, Hkv, S_cap):
+    if score.slopes is not None:
+        _need(score.slopes, torch.float32, (Hq,), "slopes")
+    if score.key_pos is not None:
+        _need(score.key_pos, torch.int32, (B, Hkv, S_cap), "key_pos")
+    if score.root_pos is not None:
+        _need(score.root_pos, torch.int32, (B,), "root_pos")
+    return _Score(float(score.cap), _ptr(score.slopes), _ptr(score.key_pos), _ptr(score.root_pos))
+
+
+def _bytes(workspace):
+    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def _cache_of(k_cache, v_cache, block_table, B, lead):
+    """(Hkv, D, rows a sequence has room for, page arguments) of caches [lead][B][Hkv][S_cap][D] or pools [lead][pages][Hkv][page][D]"""
+    if k_cache.dim() != len(lead) + 4 or tuple(k_cache.shape[:len(lead)]) != lead or \
+            (v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype)):
+        raise ValueError("inconsistent shapes of the caches")
+    first, Hkv, rows, D = (int(x) for x in k_cache.shape[len(lead):])
+    if block_table is None:
+        if first != B:
+            raise ValueError("the caches hold %d sequences, not %d" % (first, B))
+        return Hkv, D, rows, ()
+    _need(block_table, torch.int32, (B, block_table.shape[-1]), "block_table")
+    blocks = int(block_table.shape[1])
+    if blocks * rows > 0x7FFFFFFF:
+        raise ValueError("more rows than a 32-bit number counts")
+    return Hkv, D, blocks * rows, (_ptr(block_table), blocks, rows, first)
+
+
+def _tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, block_table, cache_len, parent, max_cache_len, score, out, lse, scale, status,
+                      workspace):
+    B, N, Hq, _ = q.shape
+    Hkv, D, S_cap, pages = _cache_of(k_cache, v_cache, block_table, B, ())
+    for t, what in ((k_tree, "k_tree"), (v_tree, "v_tree")):
+        _need(t, q.dtype, (B, N, Hkv, D), what)
+    _need(q, k_cache.dtype, (B, N, Hq, D), "q")
+    _need(out, q.dtype, q.shape, "out")
+    _need(cache_len, torch.int32, (B,), "cache_len")
+    _need(parent, torch.int32, (B, N), "parent")
+    if lse is not None:
+        _need(lse, torch.float32, (B, N, Hq), "lse")
+    if status is not None:
+        _need(status, torch.int32, (B,), "status")
+    shape, sc = AttnShape(B, Hq, Hkv, D, N, S_cap, _dtype_code(q)), _score(score, B, Hq, Hkv, S_cap)
+    _one_device(q, k_tree, v_tree, k_cache, v_cache, block_table, cache_len, parent, out, lse, status, workspace, *score[1:])
+    entry = lib().s4c_tree_attn_scored_paged if pages else lib().s4c_tree_attn_scored
+    _check(entry(C.byref(shape), C.byref(sc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), *pages, _ptr(cache_len),
+                 _ptr(parent), int(max_cache_len), float(scale), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), _bytes(workspace),
+                 _stream()))
+    return out
+
+
+def s4c_tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, max_cache_len: int, score: Score, out: torch.Tensor,
+                         lse: Optional[torch.Tensor] = None, scale: float = 0.0, status: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """s4c_tree_attn with changed scores; writes ``lse`` [B][N][Hq] (fp32) if it is given, and returns ``out``."""
+    cap, slopes, key_pos, root_pos = score
+    if _taken((_nat or _native()).tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, None, cache_len, parent, max_cache_len, cap, slopes,
+                                                   key_pos, root_pos, out, lse, scale, status, workspace)):
+        return out
+    return _tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, None, cache_len, parent, max_cache_len, score, out, lse, scale, status,
+                             workspace)
+
+
+def s4c_tree_attn_scored_paged(q, k_tree, v_tree, k_pool, v_pool, block_table, cache_len, parent, max_cache_len: int, score: Score,
+                               out: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
+                               status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The same over pools [num_pages][Hkv][page_size][D] behind block_table [B][max_blocks]."""
+    if block_table is None:
+        raise TypeError("block_table must be int32 [B][max_blocks]")
+    cap, slopes, key_pos, root_pos = score
+    if _taken((_nat or _native()).tree_attn_scored(q, k_tree, v_tree, k_pool, v_pool, block_table, cache_len, parent, max_cache_len, cap,
+                                                   slopes, key_pos, root_pos, out, lse, scale, status, workspace)):
+        return out
+    return _tree_attn_scored(q, k_tree, v_tree, k_pool, v_pool, block_table, cache_len, parent, max_cache_len, score, out, lse, scale, status,
+                             workspace)
+
+
+def _kv_weigh(q, k_cache, block_table, lse, cache_len, path, accept_len, max_cache_len, score, weight_in, weight, scale, status):
+    cap, slopes, key_pos, root_pos = score
+    if _taken((_nat or _native()).kv_weigh(q, k_cache, block_table, lse, cache_len, path, accept_len, max_cache_len, cap, slopes, key_pos,
+                                           root_pos, weight_in, weight, scale, status)):
+        return
+    B, N, Hq, _ = q.shape
+    Hkv, D, S_cap, pages = _cache_of(k_cache, None, block_table, B, ())
+    _need(q, k_cache.dtype, (B, N, Hq, D), "q")
+    _need(lse, torch.float32, (B, N, Hq), "lse")
+    _need(cache_len, torch.int32, (B,), "cache_len")
+    _need(accept_len, torch.int32, (B,), "accept_len")
+    _need(path, torch.int32, (B, path.shape[-1]), "path")
+    for t, what in ((weight_in, "weight_in"), (weight, "weight")):
+        _need(t, torch.float32, (B, Hkv, S_cap), what)
+    if status is not None:
+        _need(status, torch.int32, (B,), "status")
+    shape, sc = AttnShape(B, Hq, Hkv, D, N, S_cap, _dtype_code(q)), _score(score, B, Hq, Hkv, S_cap)
+    _one_device(q, k_cache, block_table, lse, cache_len, path, accept_len, weight_in, weight, status, *score[1:])
+    entry = lib().s4c_kv_weigh_paged if pages else lib().s4c_kv_weigh
+    _check(entry(C.byref(shape), C.byref(sc), _ptr(q), _ptr(k_cache), *pages, _ptr(lse), _ptr(cache_len), _ptr(path), _ptr(accept_len),
+                 int(path.shape[1]), int(max_cache_len), float(scale), _ptr(weight_in), _ptr(weight), _ptr(status), _stream()))
+
+
+def s4c_kv_weigh(q, k_cache, lse, cache_len, path, accept_len, max_cache_len: int, score: Score, weight_in, weight, scale: float = 0.0,
+                 status: Optional[torch.Tensor] = None) -> None:
+    """Adds to every cache row's total (weight_in -> weight, [B][Hkv][S_cap] fp32, the same tensor or two) the attention weight that the accepted
+    path's rows gave it; writes the positions of the path's rows into score.key_pos."""
+    _kv_weigh(q, k_cache, None, lse, cache_len, path, accept_len, max_cache_len, score, weight_in, weight, scale, status)
+
+
+def s4c_kv_weigh_paged(q, k_pool, block_table, lse, cache_len, path, accept_len, max_cache_len: int, score: Score, weight_in, weight,
+                       scale: float = 0.0, status: Optional[torch.Tensor] = None) -> None:
+    if block_table is None:
+        raise TypeError("block_table must be int32 [B][max_blocks]")
+    _kv_weigh(q, k_pool, block_table, lse, cache_len, path, accept_len, max_cache_len, score, weight_in, weight, scale, status)
+
+
+def s4c_kv_evict_workspace_size(layers: int, B: int, Hkv: int, budget: int, S_cap: int) -> int:
+    return int(lib().s4c_kv_evict_workspace_size(layers, B, Hkv, budget, S_cap))
+
+
+def _kv_evict(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight, key_pos, new_len, workspace,
+              kept, status):
+    if _taken((_nat or _native()).kv_evict(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight,
+                                           key_pos, new_len, workspace, kept, status)):
+        return
+    B = int(cache_len.shape[0]) if cache_len.dim() == 1 else -1
+    layers = int(k_cache.shape[0])
+    Hkv, D, S_cap, pages = _cache_of(k_cache, v_cache, block_table, B, (layers,))
+    for t, dtype, what in ((weight_in, torch.float32, "weight_in"), (weight, torch.float32, "weight"),
+                           (key_pos_in, torch.int32, "key_pos_in"), (key_pos, torch.int32, "key_pos")):
+        _need(t, dtype, (layers, B, Hkv, S_cap), what)
+    for t, what in ((cache_len, "cache_len"), (next_pos, "next_pos"), (new_len, "new_len")) + (((status, "status"),) if status is not None else ()):
+        _need(t, torch.int32, (B,), what)
+    if kept is not None:
+        _need(kept, torch.int32, (layers, B, Hkv, budget), "kept")
+    shape = AttnShape(B, Hkv, Hkv, D, 1, S_cap, _dtype_code(k_cache))
+    _one_device(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, weight, key_pos, new_len, workspace, kept, status)
+    entry = lib().s4c_kv_evict_paged if pages else lib().s4c_kv_evict
+    _check(entry(C.byref(shape), layers, _ptr(k_cache), _ptr(v_cache), *pages, _ptr(weight_in), _ptr(key_pos_in), _ptr(cache_len),
+                 _ptr(next_pos), int(budget), int(recent), _ptr(weight), _ptr(key_pos), _ptr(new_len), _ptr(kept), _ptr(status),
+                 _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def s4c_kv_evict(k_cache, v_cache, weight_in, key_pos_in, cache_len, next_pos, budget: int, recent: int, weight, key_pos, new_len,
+                 workspace: torch.Tensor, kept: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """Cuts caches [layers][B][Hkv][S_cap][D] down to ``budget`` rows: the most recent ones and those of the largest totals.  weight_in -> weight and
+    key_pos_in -> key_pos are [layers][B][Hkv][S_cap], cache_len -> new_len [B], each the same tensor or two."""
+    _kv_evict(k_cache, v_cache, None, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight, key_pos, new_len, workspace, kept,
+              status)
+
+
+def s4c_kv_evict_paged(k_pool, v_pool, block_table, weight_in, key_pos_in, cache_len, next_pos, budget: int, recent: int, weight, key_pos,
+                       new_len, workspace: torch.Tensor, kept: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None) -> None:
+    """The same for pools [layers][num_pages][Hkv][page_size][D] behind block_table [B][max_blocks]."""
+    if block_table is None:
+        raise TypeError("block_table must be int32 [B][max_blocks]")
+    _kv_evict(k_pool, v_pool, block_table, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight, key_pos, new_len, workspace,
+              kept, status)
 
 
 def alloc_workspace(nbytes: int, device="cuda") -> Optional[torch.Tensor]:

@@ -13,9 +13,10 @@ namespace merge {
 constexpr int kRows = 8;            // rows per workgroup and pass
 constexpr int kBatch = 8;           // partial outputs in flight together
 
-// rows [(chunk * passes) * kRows ..) of one unit, by a workgroup of 256 threads
-template <typename T, int D>
-__device__ __forceinline__ void merge_rows(const AttnArgs& a, int unit, int chunk, int passes) {
+// rows [(chunk * passes) * kRows ..) of one unit, by a workgroup of 256 threads; row_done(row, m, l): told of every merged row's
+// maximum and sum
+template <typename T, int D, class RowDone = work::NoRowDone>
+__device__ __forceinline__ void merge_rows(const AttnArgs& a, int unit, int chunk, int passes, RowDone row_done = {}) {
     constexpr int VW = D / 32;                                   // floats per lane
     const int sub = threadIdx.x & 31;
     const int b = unit / a.Hkv, kvh = unit - b * a.Hkv;
@@ -69,7 +70,9 @@ __device__ __forceinline__ void merge_rows(const AttnArgs& a, int unit, int chun
         }
         const float inv = (l > 0.f) ? 1.f / l : 0.f;
         const int node = r / a.G, g = r - node * a.G;
-        T* dst = (T*)a.out + (((size_t)b * a.N + node) * a.Hq + (kvh * a.G + g)) * D + sub * VW;
+        const size_t row = ((size_t)b * a.N + node) * a.Hq + (kvh * a.G + g);
+        if (sub == 0) row_done(row, m, l);
+        T* dst = (T*)a.out + row * D + sub * VW;
         T packed[VW];
 #pragma unroll
         for (int j = 0; j < VW; ++j) packed[j] = from_f32<T>(o[j] * inv);

@@ -75,8 +75,9 @@ __device__ __forceinline__ void put_empty(const AttnArgs& a, int team, int block
 
 // ---- A wave merges SLABS slabs of a row block of one unit from number `slab` on, its parts in the order of the runs => deterministic.
 // BATCH parts are in flight together (4 SLABS + 2 registers each).
-template <int D, Elem E, Merge MERGE, int SLABS, int BATCH>
-__device__ __forceinline__ void take(const AttnArgs& a, int unit, int block, int slab) {
+// `row_done(row, m, l)`: told the maximum and the sum of every row of the output, once.
+template <int D, Elem E, Merge MERGE, int SLABS, int BATCH, class RowDone = work::NoRowDone>
+__device__ __forceinline__ void take(const AttnArgs& a, int unit, int block, int slab, RowDone row_done = {}) {
     typedef Region<D> R;
     constexpr int kPolicy = MERGE == kHere ? kCoherent : 0;
     const int lane = threadIdx.x & 63, n = a.split;
@@ -136,7 +137,8 @@ __device__ __forceinline__ void take(const AttnArgs& a, int unit, int block, int
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const int node = r / a.G, g = r - node * a.G;
-    const size_t o0 = (((size_t)b * a.N + node) * a.Hq + kvh * a.G + g) * D + 8 * slab + 4 * (lane >> 5);
+    const size_t row = ((size_t)b * a.N + node) * a.Hq + kvh * a.G + g, o0 = row * D + 8 * slab + 4 * (lane >> 5);
+    if (slab == 0 && lane < 32) row_done(row, m, l);
 #pragma unroll
     for (int q = 0; q < SLABS; ++q) store_out<E>(a.out, o0 + 8 * q, o[q] * inv);
 }
@@ -192,8 +194,8 @@ __device__ __forceinline__ void begin(const AttnArgs& a, int team, int mt) {    
 }
 // The end of a workgroup: `part()` writes its waves' parts; then its share of the unit's merge, if it has one.  Waves of BLOCKS row
 // blocks; smem: free once every wave is here.
-template <int D, Elem E, Merge MERGE, int WAVES, int BLOCKS, class Part>
-__device__ __forceinline__ void finish(const AttnArgs& a, int team, int mt, unsigned char* smem, Part part) {
+template <int D, Elem E, Merge MERGE, int WAVES, int BLOCKS, class Part, class RowDone = work::NoRowDone>
+__device__ __forceinline__ void finish(const AttnArgs& a, int team, int mt, unsigned char* smem, Part part, RowDone row_done = {}) {
     if constexpr (MERGE == kNext) {
         part();
         return;
@@ -222,7 +224,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, int team, int mt, unsi
     auto share = [&](auto slabs, auto batch) __attribute__((always_inline)) {
         constexpr int kSlabs = decltype(slabs)::value, kTasks = D / 8 / kSlabs;
         for (int t = wave * stay + rank; t < blocks * kTasks; t += stay * WAVES)
-            take<D, E, kHere, kSlabs, decltype(batch)::value>(a, unit, mt * BLOCKS + t / kTasks, t % kTasks * kSlabs);
+            take<D, E, kHere, kSlabs, decltype(batch)::value>(a, unit, mt * BLOCKS + t / kTasks, t % kTasks * kSlabs, row_done);
     };
     if (a.split <= 8) share(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
     else share(std::integral_constant<int, 1>{}, std::integral_constant<int, kMostRuns>{});

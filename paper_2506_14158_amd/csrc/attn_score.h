@@ -1,0 +1,128 @@
+// Changed scores of the attention kernels (s4c_tree_attn_scored) and the log-sum-exp of a row.
+//
+//   x = scale q.k;   cap > 0: x <- cap tanh(x / cap);   slopes: x <- x + slope[head] (position of the key - position of the root)
+//
+// In log2 units throughout.  The distance is counted from the root and not from the row's node: the difference is the same for all
+// keys of a row, and the softmax does not see it.  The cap is where the work is: a tile's scores are C y p(y^2) with y = x / cap, C =
+// cap log2(e) and p the fifth-order fit of tanh(y)/y on |y| <= 0.6 (relative error 7.5e-8, least at Chebyshev nodes), seven operations a
+// score without a transcendental one, which run at a quarter of the rate.  Where some score of the wave lies beyond, those are
+// C - 2 C / (1 + exp2(2 log2(e) y)), off by C 2^-23, a relative 2.2e-7 there.
+// Positions are differences of 32-bit integers first and fp32 after: exact up to 2^24.
+#pragma once
+#include "common.h"
+
+#include "attn_parts.h"
+
+namespace s4c {
+namespace score {
+
+using mfma::f32x16;
+using mfma::f32x4;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kFitUpTo = 0.6f;
+constexpr float kFit[5] = {0.99999993f, -0.33332323f, 0.13310358f, -0.05210962f, 0.01548669f};
+
+// tanh(y), |y| <= kFitUpTo, times c
+__device__ __forceinline__ float fitted(float y, float c) {
+    const float z = y * y;
+    float p = fmaf(z, kFit[4] * c, kFit[3] * c);
+    p = fmaf(z, p, kFit[2] * c);
+    p = fmaf(z, p, kFit[1] * c);
+    p = fmaf(z, p, kFit[0] * c);
+    return y * p;
+}
+__device__ __forceinline__ float beyond(float y, float c) {
+    const float e = fast_exp2(y * (2.f * kLog2e));       // infinity: the cap
+    return fmaf(-2.f * c, __builtin_amdgcn_rcpf(1.f + e), c);
+}
+
+// products -> capped scores in log2 units; N values, V(j) a reference to the j-th
+template <int N, class V>
+__device__ __forceinline__ void change_all(V s, const Args<kChanged>& a, float scale_log2) {
+    if (a.cap_log2 > 0.f) {
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            s(j) *= a.to_y;
+            most = fmaxf(most, fabsf(s(j)));
+        }
+        if (!__any(most > kFitUpTo)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) s(j) = fitted(s(j), a.cap_log2);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) s(j) = fabsf(s(j)) <= kFitUpTo ? fitted(s(j), a.cap_log2) : beyond(s(j), a.cap_log2);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s(j) *= scale_log2;
+    }
+}
+// ... of a tile of 32 keys (a lane's register j), and of NG blocks of 16 x 16
+__device__ __forceinline__ void change(f32x16& s, const Args<kChanged>& a, float scale_log2) {
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = s[j];
+    change_all<16>([&](int j) -> float& { return x[j]; }, a, scale_log2);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[j] = x[j];
+}
+template <int NG>
+__device__ __forceinline__ void change(f32x4 (&s)[NG], const Args<kChanged>& a, float scale_log2) {
+    float x[4 * NG];
+#pragma unroll
+    for (int j = 0; j < 4 * NG; ++j) x[j] = s[j >> 2][j & 3];
+    change_all<4 * NG>([&](int j) -> float& { return x[j]; }, a, scale_log2);
+#pragma unroll
+    for (int j = 0; j < 4 * NG; ++j) s[j >> 2][j & 3] = x[j];
+}
+
+// Register j of a lane is key 8 (j/4) + j%4 of the lane's part of a tile.
+// ... whose first key is row `first` before (< 0) or behind the root
+__device__ __forceinline__ void add_rows(f32x16& s, float slope, int first) {
+    const float f = (float)first;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[j] = fmaf(slope, f + (float)(8 * (j >> 2) + (j & 3)), s[j]);
+}
+// ... whose positions lie in LDS
+__device__ __forceinline__ void add_looked_up(f32x16& s, float slope, const int32_t* pos, int root) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const i32x4 p = *(const i32x4*)(pos + 8 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, (float)(p[e] - root), s[4 * q + e]);
+    }
+}
+// ... of nodes of the tree
+__device__ __forceinline__ void add_depths(f32x16& s, float slope, const float* depth) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f32x4 d = *(const f32x4*)(depth + 8 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, d[e], s[4 * q + e]);
+    }
+}
+// every node's depth, by the thread that has written its ancestors
+__device__ __forceinline__ void note_depth(const AttnArgs& a, const uint32_t* anc, float* depth) {
+    const int i = threadIdx.x;
+    if (i < a.N) {
+        const uint4 m = *(const uint4*)(anc + 4 * i);
+        depth[i] = (float)(__popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w) - 1);
+    }
+}
+
+// Writes a row's log-sum-exp (natural) from its reference m (log2 units) and sum l of 2^(x - m + shift); a row without any (a flagged
+// sequence) has +infinity, so that exp(x - lse) is 0.
+struct Writer {
+    float* lse;
+    float shift;
+    __device__ __forceinline__ void operator()(size_t row, float m, float l) const {
+        if (lse) lse[row] = l > 0.f ? (m - shift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : INFINITY;
+    }
+};
+__device__ __forceinline__ work::NoRowDone writer(const Args<kPlain>&, float) { return {}; }
+__device__ __forceinline__ Writer writer(const Args<kChanged>& a, float shift) { return {a.lse, shift}; }
+
+}  // namespace score
+}  // namespace s4c

@@ -76,6 +76,9 @@ struct Order {
     }
 };
 
+// For who asks nothing about the rows of an output (others: attn_score.h).
+struct NoRowDone { __device__ __forceinline__ void operator()(size_t, float, float) const {} };
+
 // ---- what a workgroup needs to know about a sequence besides its length (each wavefront finds out by itself: no barrier)
 // parent[] (in LDS) is not a tree
 __device__ __forceinline__ bool tree_is_bad(const AttnArgs& a, const int32_t* spar) {

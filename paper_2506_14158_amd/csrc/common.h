@@ -95,6 +95,18 @@ hipError_t launch_smallm_bf16(const AttnArgs& a, const StepTail<kGreedyStep>* st
 hipError_t launch_smallm_f16(const AttnArgs& a, const StepTail<kGreedyStep>* step, hipStream_t st);
 hipError_t launch_smallm_f32(const AttnArgs& a, const StepTail<kGreedyStep>* step, hipStream_t st);
 hipError_t launch_attn_merge(const AttnArgs& a, int dtype, hipStream_t st);
+// the same with changed scores (attn_score.h)
+namespace score {
+enum Kind { kPlain = 0, kChanged = 1 };
+template <Kind KIND>
+struct Args;
+}
+hipError_t launch_tree_attn_large_scored(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
+hipError_t launch_tree_attn_small_scored(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
+hipError_t launch_large_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
+hipError_t launch_smallm_scored_bf16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
+hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
+hipError_t launch_attn_merge(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
 AttnTile attn_tile_large(const s4c_attn_shape& s);
 AttnTile attn_tile_small(const s4c_attn_shape& s, int32_t max_cache_len, int cus);
 
@@ -180,6 +192,60 @@ struct CompactArgs {
     int32_t max_blocks, page_shift, num_pages;
 };
 hipError_t launch_compact(const CompactArgs& a, hipStream_t st);
+
+// How attention scores are changed (attn_score.h), as kernels take it.
+namespace score {
+template <>
+struct Args<kPlain> {};
+template <>
+struct Args<kChanged> {
+    const float* slopes;         // [Hq] or null
+    const int32_t* key_pos;      // [B][Hkv][S_cap] or null: row j has position j, the root cache_len
+    const int32_t* root_pos;     // [B], with key_pos
+    float* lse;                  // [B][N][Hq] or null
+    float cap_log2;              // cap log2(e); 0: none
+    float to_y;                  // scale / cap
+};
+}  // namespace score
+
+struct WeighArgs {
+    const void* q;               // [B][N][Hq][D]
+    const void* k_cache;         // [B][Hkv][S_cap][D], or a pool
+    const float* lse;            // [B][N][Hq]
+    const int32_t* cache_len;    // with the path's rows
+    const int32_t* path;
+    const int32_t* accept_len;
+    const float* weight_in;      // [B][Hkv][S_cap]
+    float* weight;
+    int32_t* key_pos;            // score.key_pos, to write the path's
+    int32_t* status;
+    score::Args<score::kChanged> score;
+    float scale_log2;
+    int32_t B, Hq, Hkv, D, N, S_cap, G, max_path, max_cache_len, cus;
+    const int32_t* block_table;  // as in AttnArgs
+    int32_t max_blocks, page_shift, num_pages;
+};
+hipError_t launch_weigh(const WeighArgs& a, int dtype, hipStream_t st);
+
+struct EvictArgs {
+    void* k_cache;               // [layers][B][Hkv][S_cap][D], or pools [layers][num_pages][Hkv][page][D]
+    void* v_cache;
+    const float* weight;         // [layers][B][Hkv][S_cap]; the outputs may be the inputs
+    float* weight_out;
+    const int32_t* key_pos;
+    int32_t* key_pos_out;
+    const int32_t* cache_len;
+    int32_t* new_len;
+    const int32_t* next_pos;
+    int32_t* kept;               // [layers][B][Hkv][budget] or null
+    int32_t* status;
+    int2* meta;                  // [units] rows that move, rows that stay
+    int32_t* lists;              // [units][2][list_len] places, and the rows that move there
+    int32_t layers, B, Hkv, S_cap, budget, recent, list_len, row_bytes, cus;
+    const int32_t* block_table;
+    int32_t max_blocks, page_shift, num_pages;
+};
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
 
 struct BuildArgs {
     const void* logits;        // draft logits [B][N][V]

@@ -1,0 +1,212 @@
+// What the cache rows are worth: the attention weight that the accepted path's query rows give to every cache row, added to the rows'
+// totals (s4c_kv_weigh).  weight[j] += sum over path nodes k and the heads of a group of exp(x_kj - lse_k), x as the attention had it.
+//
+// The log-sum-exp is known, so this is one pass over K: a stream of n D elements per KV head, each feeding 2 R flops (R = path
+// nodes x heads of the group).  A wave takes NG x 16 keys: K rows go from memory straight into the B operands of 16x16 matrix
+// instructions (a lane has 16 consecutive bytes of a row; the reduction index is permuted the same way for Q), the query rows lie in LDS
+// in operand order, and the scores come out with a lane per key, so that a key's sum over the rows is additions in registers and two
+// exchanges between the wave's quarters.  No workgroup needs another's result, every sum has one order.
+#include "attn_score.h"
+
+namespace s4c {
+
+namespace {
+
+using namespace mfma;
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kChunkRows = 128;              // query rows in LDS at a time
+
+// 16-byte pieces of a row that a lane has: piece 4 t + lane / 16 of its row for t < T.
+template <typename E, int D, int NG>
+struct Tile {
+    static constexpr int kRowB = D * sizeof(E), kT = kRowB / 64, kKeys = 16 * NG;
+};
+
+template <typename E>
+__device__ __forceinline__ f32x4 product(uint4 q, uint4 k, f32x4 c) {
+    if constexpr (sizeof(E) == 4) {
+        const f32x4 x = __builtin_bit_cast(f32x4, q), y = __builtin_bit_cast(f32x4, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+        return c;
+    } else {
+        return mma16<std::is_same<E, f16_t>::value>(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, k), c);
+    }
+}
+
+template <typename E, int D, int NG, bool PAGED>
+__global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
+    typedef Tile<E, D, NG> T;
+    __shared__ __attribute__((aligned(16))) unsigned char s_q[kChunkRows * T::kRowB];     // [16-row block][piece t][lane] 16 bytes
+    __shared__ __attribute__((aligned(16))) float s_lse[kChunkRows], s_slope[kChunkRows];
+    __shared__ int s_node[kChunkRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int unit = blockIdx.x, b = unit / a.Hkv, kvh = unit - b * a.Hkv;
+    const int n = a.cache_len[b], L = a.accept_len[b];
+    const int32_t* path = a.path + (size_t)b * a.max_path;
+
+    // ---- is everything the sequence's?  (every workgroup finds the same)
+    bool bad = n < 1 || n > a.max_cache_len || n > a.S_cap || L < 0 || L >= a.max_path || L + 1 > n;
+    if (!bad) {
+        for (int k = tid; k <= L; k += kThreads) bad = bad || path[k] < 0 || path[k] >= a.N;
+        if constexpr (PAGED)
+            for (int i = tid; i < (n + (1 << a.page_shift) - 1) >> a.page_shift; i += kThreads) {
+                const int id = a.block_table[(size_t)b * a.max_blocks + i];
+                bad = bad || id < 0 || id >= a.num_pages;
+            }
+    }
+    bad = __syncthreads_or(bad) != 0;
+    if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
+    if (bad) return;
+
+    const int first = n - (L + 1), R = (L + 1) * a.G, chunks = (R + kChunkRows - 1) / kChunkRows;
+    // this workgroup's keys, in steps of all its waves' tiles
+    constexpr int kStep = kWaves * T::kKeys;
+    const int steps = (n + kStep - 1) / kStep, per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int step0 = blockIdx.y * per, step1 = min(steps, step0 + per);
+    if (step0 >= step1) return;
+
+    // query rows c kChunkRows .. into LDS
+    auto stage = [&](int c) {
+        const int r0 = c * kChunkRows, rows = min(kChunkRows, R - r0), up = (rows + 15) / 16 * 16;
+        for (int r = tid; r < up; r += kThreads) {
+            const int k = min(r0 + r, R - 1) / a.G, g = min(r0 + r, R - 1) - k * a.G, node = path[k];
+            const size_t at = ((size_t)b * a.N + node) * a.Hq + kvh * a.G + g;
+            s_node[r] = (int)k;
+            s_lse[r] = r < rows ? a.lse[at] * kLog2e : INFINITY;
+            s_slope[r] = a.score.slopes ? a.score.slopes[kvh * a.G + g] * kLog2e : 0.f;
+        }
+        for (int e = tid; e < up * (T::kRowB / 16); e += kThreads) {
+            const int r = e / (T::kRowB / 16), piece = e % (T::kRowB / 16);
+            const int rr = min(r0 + r, R - 1), k = rr / a.G, g = rr - k * a.G, node = path[k];
+            const uint4 v = *(const uint4*)((const unsigned char*)a.q + (((size_t)b * a.N + node) * a.Hq + kvh * a.G + g) * T::kRowB + piece * 16);
+            *(uint4*)(s_q + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = v;
+        }
+    };
+
+    const int root = a.score.key_pos ? a.score.root_pos[b] : first;
+    const size_t row0 = ((size_t)b * a.Hkv + kvh) * a.S_cap;           // of the totals and positions
+    uint4 kf[NG][T::kT], nf[NG][T::kT];
+    int pos[NG], npos[NG];
+    float total, ntotal;
+    auto fetch = [&](int step, uint4 (&f)[NG][T::kT], int (&p)[NG], float& w) __attribute__((always_inline)) {
+        const int j0 = __builtin_amdgcn_readfirstlane(step * kStep + wave * T::kKeys);
+        size_t row = row0 + j0;
+        if constexpr (PAGED) {
+            const int jc = min(j0, n - 1) & ~(T::kKeys - 1);
+            row = (((size_t)a.block_table[(size_t)b * a.max_blocks + (jc >> a.page_shift)] * a.Hkv + kvh) << a.page_shift) + (jc & ((1 << a.page_shift) - 1));
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const int in = 16 * g + (lane & 15);
+            const int j = min(j0 + in, n - 1);
+            // (a tile behind the last key: the last one's rows; never multiplied into anything that is kept)
+            const int off = PAGED ? j - (min(j0, n - 1) & ~(T::kKeys - 1)) : j - j0;
+            const unsigned char* src = (const unsigned char*)a.k_cache + (ptrdiff_t)(row + (ptrdiff_t)off) * T::kRowB + (lane >> 4) * 16;
+#pragma unroll
+            for (int t = 0; t < T::kT; ++t) f[g][t] = *(const uint4*)(src + 64 * t);
+            p[g] = a.score.slopes && a.score.key_pos ? a.score.key_pos[row0 + j] : j;
+        }
+        w = a.weight_in[row0 + min(j0 + (lane & (T::kKeys - 1)), n - 1)];
+    };
+
+    fetch(step0, nf, npos, ntotal);
+    if (chunks == 1) {
+        stage(0);
+        __syncthreads();
+    }
+    for (int step = step0; step < step1; ++step) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int t = 0; t < T::kT; ++t) kf[g][t] = nf[g][t];
+            pos[g] = npos[g];
+        }
+        total = ntotal;
+        if (step + 1 < step1) fetch(step + 1, nf, npos, ntotal);
+        const int j0 = step * kStep + wave * T::kKeys;
+        const bool own_rows = j0 + T::kKeys > first;                   // some keys are the path's own
+        float rel[NG], sum[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const int j = j0 + 16 * g + (lane & 15);
+            rel[g] = (float)(j >= first ? j - first : pos[g] - root);
+            sum[g] = 0.f;
+        }
+        for (int c = 0; c < chunks; ++c) {
+            if (chunks > 1) {
+                __syncthreads();
+                stage(c);
+                __syncthreads();
+            }
+            const int blocks = (min(kChunkRows, R - c * kChunkRows) + 15) / 16;
+            for (int blk = 0; blk < blocks; ++blk) {
+                f32x4 s[NG];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) s[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < T::kT; ++t) {
+                    const uint4 q = *(const uint4*)(s_q + ((blk * T::kT + t) * 64 + lane) * 16);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) s[g] = product<E>(q, kf[g][t], s[g]);
+                }
+                const int r4 = blk * 16 + 4 * (lane >> 4);
+                const f32x4 lse = *(const f32x4*)(s_lse + r4), slope = *(const f32x4*)(s_slope + r4);
+                score::change<NG>(s, a.score, a.scale_log2);
+                if (a.score.slopes) {
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[g][e] = fmaf(slope[e], rel[g], s[g][e]);
+                }
+                if (own_rows) {
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (j0 + 16 * g + (lane & 15) > first + s_node[r4 + e]) s[g][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(s[g][e] - lse[e]);
+            }
+        }
+        // lane 16 g + i has key 16 g + i of the tile
+        float mine = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            sum[g] += __shfl_xor(sum[g], 16);
+            sum[g] += __shfl_xor(sum[g], 32);
+            if ((lane >> 4) == g) mine = sum[g];
+        }
+        const int j = j0 + lane;
+        if (lane < T::kKeys && j < n) {
+            a.weight[row0 + j] = j < first ? total + mine : mine;
+            if (a.score.key_pos && j >= first) a.key_pos[row0 + j] = root + (j - first);
+        }
+    }
+}
+
+template <typename E, int D, int NG>
+hipError_t launch(const WeighArgs& a, hipStream_t st) {
+    const int units = a.B * a.Hkv, step = kWaves * 16 * NG;
+    const int steps = (a.max_cache_len + step - 1) / step;
+    int runs = (2 * 2 * a.cus + units - 1) / units;
+    if (runs > steps) runs = steps < 1 ? 1 : steps;
+    const dim3 grid((unsigned)units, (unsigned)runs);
+    if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false>), grid, dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_weigh(const WeighArgs& a, int dtype, hipStream_t st) {
+    if (dtype == S4C_F32) return a.D == 64 ? launch<float, 64, 4>(a, st) : launch<float, 128, 2>(a, st);
+    if (dtype == S4C_F16) return a.D == 64 ? launch<f16_t, 64, 4>(a, st) : launch<f16_t, 128, 4>(a, st);
+    return a.D == 64 ? launch<bf16_t, 64, 4>(a, st) : launch<bf16_t, 128, 4>(a, st);
+}
+
+}  // namespace s4c

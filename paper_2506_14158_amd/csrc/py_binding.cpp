@@ -403,10 +403,134 @@ PyObject* verify_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return launch(s4c_verify_step, &p, stream());
 }
 
+// ---- changed scores, and a cache that rows are evicted from
+// All of a call's tensors are on the current device, whose stream it goes to.
+void here(Args& a, std::initializer_list<const Tensor*> tensors) {
+    if (!a.ok) return;
+    const auto device = c10::hip::current_device();
+    for (const Tensor* t : tensors) a.need(!t || t->get_device() == device);
+}
+// caches [B][Hkv][S_cap][D] or, behind a block table [B][blocks], pools [pages][Hkv][page][D], with `lead` dimensions before them
+struct Cache { int64_t first, Hkv, rows, D, S_cap; };
+Cache cache_of(Args& a, const Tensor* kc, const Tensor* bt, int lead, int64_t B) {
+    Cache c{0, 0, 0, 0, 0};
+    if (!a.ok || kc->dim() != lead + 4) { a.ok = false; return c; }
+    c = {kc->size(lead), kc->size(lead + 1), kc->size(lead + 2), kc->size(lead + 3), kc->size(lead + 2)};
+    if (bt) {
+        a.need(bt->dim() == 2 && bt->size(0) == B);
+        if (a.ok) c.S_cap = bt->size(1) * c.rows;
+    } else a.need(c.first == B);
+    a.need(c.S_cap == (int32_t)c.S_cap && c.first == (int32_t)c.first);
+    return c;
+}
+// (cap, slopes, key_pos, root_pos) from argument i on
+struct ScoreTensors { s4c_score s; const Tensor *slopes, *pos, *root; };
+ScoreTensors score_of(Args& a, int i, int64_t B, int64_t Hq, int64_t Hkv, int64_t S_cap) {
+    ScoreTensors t{{}, a.maybe(i + 1, F32), a.maybe(i + 2, I32), a.maybe(i + 3, I32)};
+    t.s.cap = a.real(i);
+    if (t.slopes) a.shape(t.slopes, {Hq});
+    if (t.pos) a.shape(t.pos, {B, Hkv, S_cap});
+    if (t.root) a.shape(t.root, {B});
+    if (!a.ok) return t;
+    t.s.slopes = (const float*)ptr(t.slopes); t.s.key_pos = (int32_t*)ptr(t.pos); t.s.root_pos = (const int32_t*)ptr(t.root);
+    return t;
+}
+
+// (q, k_tree, v_tree, k_cache, v_cache, block_table, cache_len, parent, max_cache_len, cap, slopes, key_pos, root_pos, out, lse, scale, status,
+//  workspace)
+PyObject* tree_attn_scored(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a(v, n, 18);
+    AttnTensors t = attn_tensors(a, 0, 1, 3, 13);
+    const Tensor *bt = a.maybe(5, I32), *len = a.tensor(6, I32), *par = a.tensor(7, I32), *lse = a.maybe(14, F32), *status = a.maybe(16, I32),
+                 *ws = a.maybe(17);
+    const long mcl = a.integer(8);
+    const float scale = a.real(15);
+    const Cache c = cache_of(a, t.kc, bt, 0, t.s.B);
+    a.need(c.Hkv == t.s.Hkv && c.D == t.s.D);
+    a.shape(len, {t.s.B});
+    a.shape(par, {t.s.B, t.s.N});
+    if (lse) a.shape(lse, {t.s.B, t.s.N, t.s.Hq});
+    if (status) a.shape(status, {t.s.B});
+    const ScoreTensors sc = score_of(a, 9, t.s.B, t.s.Hq, t.s.Hkv, c.S_cap);
+    here(a, {t.q, t.kt, t.vt, t.kc, t.vc, t.out, bt, len, par, lse, status, ws, sc.slopes, sc.pos, sc.root});
+    if (!a.ok) return answer(kNotMine);
+    t.s.S_cap = (int32_t)c.S_cap;
+    if (bt)
+        return launch(s4c_tree_attn_scored_paged, &t.s, &sc.s, ptr(t.q), ptr(t.kt), ptr(t.vt), ptr(t.kc), ptr(t.vc), (int32_t*)ptr(bt),
+                      (int32_t)bt->size(1), (int32_t)c.rows, (int32_t)c.first, (int32_t*)ptr(len), (int32_t*)ptr(par), (int32_t)mcl, scale,
+                      ptr(t.out), (float*)ptr(lse), (int32_t*)ptr(status), ptr(ws), bytes(ws), stream());
+    return launch(s4c_tree_attn_scored, &t.s, &sc.s, ptr(t.q), ptr(t.kt), ptr(t.vt), ptr(t.kc), ptr(t.vc), (int32_t*)ptr(len),
+                  (int32_t*)ptr(par), (int32_t)mcl, scale, ptr(t.out), (float*)ptr(lse), (int32_t*)ptr(status), ptr(ws), bytes(ws), stream());
+}
+
+// (q, k_cache, block_table, lse, cache_len, path, accept_len, max_cache_len, cap, slopes, key_pos, root_pos, weight_in, weight, scale, status)
+PyObject* kv_weigh(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a(v, n, 16);
+    const Tensor *q = a.tensor(0), *kc = a.tensor(1), *bt = a.maybe(2, I32), *lse = a.tensor(3, F32), *len = a.tensor(4, I32),
+                 *path = a.tensor(5, I32), *alen = a.tensor(6, I32), *win = a.tensor(12, F32), *w = a.tensor(13, F32), *status = a.maybe(15, I32);
+    const long mcl = a.integer(7);
+    const float scale = a.real(14);
+    const int dt = dtype(a, q);
+    if (!a.ok || q->dim() != 4 || path->dim() != 2) return answer(kNotMine);
+    const int64_t B = q->size(0), N = q->size(1), Hq = q->size(2), D = q->size(3);
+    const Cache c = cache_of(a, kc, bt, 0, B);
+    a.need(c.D == D);
+    if (!a.ok) return answer(kNotMine);
+    a.need(kc->scalar_type() == q->scalar_type());
+    a.shape(lse, {B, N, Hq});
+    a.shape(len, {B});
+    a.shape(alen, {B});
+    a.need(path->size(0) == B);
+    a.shape(win, {B, c.Hkv, c.S_cap});
+    a.shape(w, {B, c.Hkv, c.S_cap});
+    if (status) a.shape(status, {B});
+    const ScoreTensors sc = score_of(a, 8, B, Hq, c.Hkv, c.S_cap);
+    here(a, {q, kc, bt, lse, len, path, alen, win, w, status, sc.slopes, sc.pos, sc.root});
+    if (!a.ok) return answer(kNotMine);
+    const s4c_attn_shape s = {(int32_t)B, (int32_t)Hq, (int32_t)c.Hkv, (int32_t)D, (int32_t)N, (int32_t)c.S_cap, dt};
+    if (bt)
+        return launch(s4c_kv_weigh_paged, &s, &sc.s, ptr(q), ptr(kc), (int32_t*)ptr(bt), (int32_t)bt->size(1), (int32_t)c.rows, (int32_t)c.first,
+                      (float*)ptr(lse), (int32_t*)ptr(len), (int32_t*)ptr(path), (int32_t*)ptr(alen), (int32_t)path->size(1), (int32_t)mcl, scale,
+                      (float*)ptr(win), (float*)ptr(w), (int32_t*)ptr(status), stream());
+    return launch(s4c_kv_weigh, &s, &sc.s, ptr(q), ptr(kc), (float*)ptr(lse), (int32_t*)ptr(len), (int32_t*)ptr(path), (int32_t*)ptr(alen),
+                  (int32_t)path->size(1), (int32_t)mcl, scale, (float*)ptr(win), (float*)ptr(w), (int32_t*)ptr(status), stream());
+}
+
+// (k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight, key_pos, new_len, workspace, kept, status)
+PyObject* kv_evict(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a(v, n, 15);
+    const Tensor *kc = a.tensor(0), *vc = a.tensor(1), *bt = a.maybe(2, I32), *win = a.tensor(3, F32), *pin = a.tensor(4, I32),
+                 *len = a.tensor(5, I32), *next = a.tensor(6, I32), *w = a.tensor(9, F32), *pos = a.tensor(10, I32), *nlen = a.tensor(11, I32),
+                 *ws = a.maybe(12), *kept = a.maybe(13, I32), *status = a.maybe(14, I32);
+    const long budget = a.integer(7), recent = a.integer(8);
+    const int dt = dtype(a, kc);
+    if (!a.ok || kc->dim() != 5 || len->dim() != 1) return answer(kNotMine);
+    const int64_t layers = kc->size(0), B = len->size(0);
+    const Cache c = cache_of(a, kc, bt, 1, B);
+    a.same(vc, kc);
+    for (const Tensor* t : {win, pin, w, pos}) a.shape(t, {layers, B, c.Hkv, c.S_cap});
+    a.shape(next, {B});
+    a.shape(nlen, {B});
+    if (kept) a.shape(kept, {layers, B, c.Hkv, budget});
+    if (status) a.shape(status, {B});
+    here(a, {kc, vc, bt, win, pin, len, next, w, pos, nlen, ws, kept, status});
+    if (!a.ok || layers != (int32_t)layers) return answer(kNotMine);
+    const s4c_attn_shape s = {(int32_t)B, (int32_t)c.Hkv, (int32_t)c.Hkv, (int32_t)c.D, 1, (int32_t)c.S_cap, dt};
+    if (bt)
+        return launch(s4c_kv_evict_paged, &s, (int32_t)layers, ptr(kc), ptr(vc), (int32_t*)ptr(bt), (int32_t)bt->size(1), (int32_t)c.rows,
+                      (int32_t)c.first, (float*)ptr(win), (int32_t*)ptr(pin), (int32_t*)ptr(len), (int32_t*)ptr(next), (int32_t)budget,
+                      (int32_t)recent, (float*)ptr(w), (int32_t*)ptr(pos), (int32_t*)ptr(nlen), (int32_t*)ptr(kept), (int32_t*)ptr(status),
+                      ptr(ws), bytes(ws), stream());
+    return launch(s4c_kv_evict, &s, (int32_t)layers, ptr(kc), ptr(vc), (float*)ptr(win), (int32_t*)ptr(pin), (int32_t*)ptr(len),
+                  (int32_t*)ptr(next), (int32_t)budget, (int32_t)recent, (float*)ptr(w), (int32_t*)ptr(pos), (int32_t*)ptr(nlen),
+                  (int32_t*)ptr(kept), (int32_t*)ptr(status), ptr(ws), bytes(ws), stream());
+}
+
 #define S4C_PY(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {S4C_PY(tree_attn), S4C_PY(tree_attn_paged), S4C_PY(accept_path), S4C_PY(accept_path_static),
                          S4C_PY(accept_resample), S4C_PY(kv_compact), S4C_PY(kv_compact_paged), S4C_PY(commit_path),
-                         S4C_PY(commit_path_paged), S4C_PY(build_tree), S4C_PY(draft_linear), S4C_PY(verify_step), {nullptr, nullptr, 0, nullptr}};
+                         S4C_PY(commit_path_paged), S4C_PY(build_tree), S4C_PY(draft_linear), S4C_PY(verify_step), S4C_PY(tree_attn_scored), S4C_PY(kv_weigh), S4C_PY(kv_evict),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_s4c_py", "libs4c's entry points on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

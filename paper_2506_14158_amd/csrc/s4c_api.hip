@@ -1,4 +1,5 @@
 // C ABI of libs4c: argument checks, launch planning, kernel launches.  See include/s4c.h.
+#include "attn_score.h"
 #include "attn_step.h"
 #include "common.h"
 #include "resample_plan.h"
@@ -744,6 +745,180 @@ s4c_status s4c_verify_step(const s4c_step* p, void* hip_stream) {
         if (e == hipSuccess) e = launch_compact(compact, st);
     }
     return e == hipSuccess ? S4C_OK : S4C_ERR_HIP;
+}
+
+#pragma GCC visibility pop
+}  // extern "C"
+
+// ---- changed scores, and a cache that rows are evicted from
+namespace {
+
+// How the scores of a call with this scale are changed; false: not a score that the kernels take.
+bool score_args(const s4c_score* sc, float scale, int32_t D, score::Args<score::kChanged>* a, s4c_status* why) {
+    *a = {};
+    if (!sc) return true;
+    if (sc->key_pos && !sc->root_pos) { *why = S4C_ERR_NULL; return false; }
+    if (!(sc->cap >= 0.f)) { *why = S4C_ERR_SHAPE; return false; }
+    if (sc->cap > 0.f) {
+        a->cap_log2 = sc->cap * kLog2e;
+        a->to_y = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) / sc->cap;
+        if (!isfinite(2.f * a->cap_log2) || !isfinite(a->to_y) || a->cap_log2 <= 0.f) { *why = S4C_ERR_SHAPE; return false; }
+    }
+    a->slopes = sc->slopes;
+    a->key_pos = sc->key_pos;
+    a->root_pos = sc->root_pos;
+    return true;
+}
+
+s4c_status tree_attn_scored_impl(const s4c_attn_shape* shape, const s4c_score* score_in, const void* q, const void* k_tree, const void* v_tree,
+                                 const void* k_cache, const void* v_cache, const int32_t* block_table, int32_t max_blocks, int32_t page_shift,
+                                 int32_t num_pages, const int32_t* cache_len, const int32_t* parent, int32_t max_cache_len, float scale,
+                                 void* out, float* lse, int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    AttnPlan p;
+    AttnArgs a;
+    const s4c_status ok = tree_attn_prepare(shape, q, k_tree, v_tree, k_cache, v_cache, block_table, max_blocks, page_shift, num_pages,
+                                            cache_len, parent, max_cache_len, scale, out, status, workspace, workspace_bytes, &p, &a);
+    if (ok != S4C_OK) return ok;
+    score::Args<score::kChanged> sc;
+    s4c_status why;
+    if (!score_args(score_in, scale, shape->D, &sc, &why)) return why;
+    if (!sc.slopes) sc.key_pos = sc.root_pos = nullptr;       // nothing depends on positions
+    sc.lse = lse;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = p.large ? launch_tree_attn_large_scored(a, shape->dtype, sc, st) : launch_tree_attn_small_scored(a, shape->dtype, sc, st);
+    if (e == hipSuccess && a.split == 0) e = launch_attn_merge(a, shape->dtype, sc, st);
+    return e == hipSuccess ? S4C_OK : S4C_ERR_HIP;
+}
+
+s4c_status weigh_impl(const s4c_attn_shape* shape, const s4c_score* score_in, const void* q, const void* k_cache, const int32_t* block_table,
+                      int32_t max_blocks, int32_t page_shift, int32_t num_pages, const float* lse, const int32_t* cache_len,
+                      const int32_t* path, const int32_t* accept_len, int32_t max_path, int32_t max_cache_len, float scale,
+                      const float* weight_in, float* weight, int32_t* status, void* hip_stream) {
+    if (!shape || !q || !k_cache || !lse || !cache_len || !path || !accept_len || !weight_in || !weight) return S4C_ERR_NULL;
+    s4c_status why;
+    if (!shape_ok(shape, &why)) return why;
+    if (max_path <= 0 || shape->S_cap <= 0 || max_cache_len <= 0 || max_cache_len > shape->S_cap) return S4C_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(k_cache)) return S4C_ERR_SHAPE;
+    if ((long long)shape->B * shape->Hkv > 0x7FFFFFFFll || (long long)max_path * shape->Hq > 0x3FFFFFFFll) return S4C_ERR_UNSUPPORTED;
+    WeighArgs a;
+    if (!score_args(score_in, scale, shape->D, &a.score, &why)) return why;
+    a.q = q; a.k_cache = k_cache; a.lse = lse; a.cache_len = cache_len; a.path = path; a.accept_len = accept_len;
+    a.weight_in = weight_in; a.weight = weight; a.key_pos = score_in ? score_in->key_pos : nullptr; a.status = status;
+    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)shape->D)) * kLog2e;
+    a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.D = shape->D; a.N = shape->N; a.S_cap = shape->S_cap;
+    a.G = shape->Hq / shape->Hkv; a.max_path = max_path; a.max_cache_len = max_cache_len; a.cus = device_cus();
+    a.block_table = block_table; a.max_blocks = max_blocks; a.page_shift = page_shift; a.num_pages = num_pages;
+    return launch_weigh(a, shape->dtype, (hipStream_t)hip_stream) == hipSuccess ? S4C_OK : S4C_ERR_HIP;
+}
+
+// rows that move in a unit, at most
+int32_t evict_list_len(int32_t budget, int32_t S_cap) { return S_cap <= budget ? 0 : budget < S_cap - budget ? budget : S_cap - budget; }
+size_t evict_meta_bytes(int32_t layers, int32_t B, int32_t Hkv) { return (((size_t)layers * B * Hkv * sizeof(int2) + 255) / 256) * 256; }
+bool evict_sizes_ok(int32_t layers, int32_t B, int32_t Hkv, int32_t budget, int32_t S_cap) {
+    return layers > 0 && layers <= 65534 && B > 0 && B <= 65535 && Hkv > 0 && Hkv <= 65535 && budget > 0 && S_cap > 0 &&
+           (long long)layers * B * Hkv <= 0x7FFFFFFFll;
+}
+
+s4c_status evict_impl(const s4c_attn_shape* shape, int32_t layers, void* k_cache, void* v_cache, const int32_t* block_table, int32_t max_blocks,
+                      int32_t page_shift, int32_t num_pages, const float* weight_in, const int32_t* key_pos_in, const int32_t* cache_len,
+                      const int32_t* next_pos, int32_t budget, int32_t recent, float* weight, int32_t* key_pos, int32_t* new_len, int32_t* kept,
+                      int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!shape || !k_cache || !v_cache || !weight_in || !key_pos_in || !cache_len || !next_pos || !weight || !key_pos || !new_len)
+        return S4C_ERR_NULL;
+    if (!evict_sizes_ok(layers, shape->B, shape->Hkv, budget, shape->S_cap) || recent < 0 || recent > budget) return S4C_ERR_SHAPE;
+    if ((shape->D != 64 && shape->D != 128) || !dtype_ok(shape->dtype)) return S4C_ERR_UNSUPPORTED;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return S4C_ERR_SHAPE;
+    const size_t need = s4c_kv_evict_workspace_size(layers, shape->B, shape->Hkv, budget, shape->S_cap);
+    if (!workspace || workspace_bytes < need || (((uintptr_t)workspace) & 255)) return S4C_ERR_WORKSPACE;
+    EvictArgs a;
+    a.k_cache = k_cache; a.v_cache = v_cache; a.weight = weight_in; a.weight_out = weight; a.key_pos = key_pos_in; a.key_pos_out = key_pos;
+    a.cache_len = cache_len; a.new_len = new_len; a.next_pos = next_pos; a.kept = kept; a.status = status;
+    a.meta = (int2*)workspace;
+    a.lists = (int32_t*)((char*)workspace + evict_meta_bytes(layers, shape->B, shape->Hkv));
+    a.layers = layers; a.B = shape->B; a.Hkv = shape->Hkv; a.S_cap = shape->S_cap; a.budget = budget; a.recent = recent;
+    a.list_len = evict_list_len(budget, shape->S_cap);
+    a.row_bytes = shape->D * (shape->dtype == S4C_F32 ? 4 : 2);
+    a.cus = device_cus();
+    a.block_table = block_table; a.max_blocks = max_blocks; a.page_shift = page_shift; a.num_pages = num_pages;
+    return launch_evict(a, (hipStream_t)hip_stream) == hipSuccess ? S4C_OK : S4C_ERR_HIP;
+}
+
+// of a paged call
+s4c_status pages_ok(const s4c_attn_shape* shape, const int32_t* block_table, int32_t max_blocks, int32_t page_size, int32_t num_pages, int* shift) {
+    if (!shape || !block_table) return S4C_ERR_NULL;
+    *shift = page_shift_of(page_size);
+    if (*shift < 0) return S4C_ERR_UNSUPPORTED;
+    if (max_blocks <= 0 || num_pages <= 0 || (long long)max_blocks * page_size > 0x7FFFFFFFll) return S4C_ERR_SHAPE;
+    return shape->S_cap == max_blocks * page_size ? S4C_OK : S4C_ERR_SHAPE;
+}
+}  // namespace
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+s4c_status s4c_tree_attn_scored(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree, const void* v_tree,
+                                const void* k_cache, const void* v_cache, const int32_t* cache_len, const int32_t* parent,
+                                int32_t max_cache_len, float scale, void* out, float* lse, int32_t* status, void* workspace,
+                                size_t workspace_bytes, void* hip_stream) {
+    return tree_attn_scored_impl(shape, score, q, k_tree, v_tree, k_cache, v_cache, nullptr, 0, 0, 0, cache_len, parent, max_cache_len, scale,
+                                 out, lse, status, workspace, workspace_bytes, hip_stream);
+}
+
+s4c_status s4c_tree_attn_scored_paged(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree,
+                                      const void* v_tree, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                                      int32_t max_blocks, int32_t page_size, int32_t num_pages, const int32_t* cache_len,
+                                      const int32_t* parent, int32_t max_cache_len, float scale, void* out, float* lse, int32_t* status,
+                                      void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!k_pool || !v_pool) return S4C_ERR_NULL;
+    int sh;
+    const s4c_status ok = pages_ok(shape, block_table, max_blocks, page_size, num_pages, &sh);
+    if (ok != S4C_OK) return ok;
+    return tree_attn_scored_impl(shape, score, q, k_tree, v_tree, k_pool, v_pool, block_table, max_blocks, sh, num_pages, cache_len, parent,
+                                 max_cache_len, scale, out, lse, status, workspace, workspace_bytes, hip_stream);
+}
+
+s4c_status s4c_kv_weigh(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_cache, const float* lse,
+                        const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path, int32_t max_cache_len,
+                        float scale, const float* weight_in, float* weight, int32_t* status, void* hip_stream) {
+    return weigh_impl(shape, score, q, k_cache, nullptr, 0, 0, 0, lse, cache_len, path, accept_len, max_path, max_cache_len, scale, weight_in,
+                      weight, status, hip_stream);
+}
+
+s4c_status s4c_kv_weigh_paged(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_pool,
+                              const int32_t* block_table, int32_t max_blocks, int32_t page_size, int32_t num_pages, const float* lse,
+                              const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path,
+                              int32_t max_cache_len, float scale, const float* weight_in, float* weight, int32_t* status, void* hip_stream) {
+    int sh;
+    const s4c_status ok = pages_ok(shape, block_table, max_blocks, page_size, num_pages, &sh);
+    if (ok != S4C_OK) return ok;
+    return weigh_impl(shape, score, q, k_pool, block_table, max_blocks, sh, num_pages, lse, cache_len, path, accept_len, max_path,
+                      max_cache_len, scale, weight_in, weight, status, hip_stream);
+}
+
+size_t s4c_kv_evict_workspace_size(int32_t layers, int32_t B, int32_t Hkv, int32_t budget, int32_t S_cap) {
+    if (!evict_sizes_ok(layers, B, Hkv, budget, S_cap)) return 0;
+    const size_t lists = (size_t)layers * B * Hkv * 2 * evict_list_len(budget, S_cap) * sizeof(int32_t);
+    return evict_meta_bytes(layers, B, Hkv) + (lists + 255) / 256 * 256;
+}
+
+s4c_status s4c_kv_evict(const s4c_attn_shape* shape, int32_t layers, void* k_cache, void* v_cache, const float* weight_in,
+                        const int32_t* key_pos_in, const int32_t* cache_len, const int32_t* next_pos, int32_t budget, int32_t recent,
+                        float* weight, int32_t* key_pos, int32_t* new_len, int32_t* kept, int32_t* status, void* workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+    return evict_impl(shape, layers, k_cache, v_cache, nullptr, 0, 0, 0, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight,
+                      key_pos, new_len, kept, status, workspace, workspace_bytes, hip_stream);
+}
+
+s4c_status s4c_kv_evict_paged(const s4c_attn_shape* shape, int32_t layers, void* k_pool, void* v_pool, const int32_t* block_table,
+                              int32_t max_blocks, int32_t page_size, int32_t num_pages, const float* weight_in, const int32_t* key_pos_in,
+                              const int32_t* cache_len, const int32_t* next_pos, int32_t budget, int32_t recent, float* weight,
+                              int32_t* key_pos, int32_t* new_len, int32_t* kept, int32_t* status, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+    int sh;
+    const s4c_status ok = pages_ok(shape, block_table, max_blocks, page_size, num_pages, &sh);
+    if (ok != S4C_OK) return ok;
+    return evict_impl(shape, layers, k_pool, v_pool, block_table, max_blocks, sh, num_pages, weight_in, key_pos_in, cache_len, next_pos, budget,
+                      recent, weight, key_pos, new_len, kept, status, workspace, workspace_bytes, hip_stream);
 }
 
 #pragma GCC visibility pop

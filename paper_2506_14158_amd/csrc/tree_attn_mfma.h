@@ -27,6 +27,7 @@
 //   * The keys are divided between teams of workgroups (attn_division.h); parts of a divided unit are written
 //     unnormalised (attn_parts.h, attn_merge.h).
 #pragma once
+#include "attn_score.h"
 #include "attn_step.h"
 
 namespace s4c {
@@ -38,10 +39,13 @@ using namespace mfma;
 constexpr int kBN = 64;                     // keys per tile
 constexpr float kLazyLog2 = 8.0f;           // full tiles rescale only when a row maximum grew by more than 2^8
 constexpr int lds_bytes_for(int ns, int d) { return ns * 2 * kBN * d * 2 + kMaxNodes * 16 + kMaxNodes * 4; }
+// with changed scores behind it: positions of the ring's keys, slopes of every wave's rows, depths of the nodes
+constexpr int scored_lds_bytes_for(int ns, int d, int wr) { return lds_bytes_for(ns, d) + ns * kBN * 4 + wr * 256 + kMaxNodes * 4; }
 
-template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, parts::Merge MERGE>
+template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
-void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
+void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
+    constexpr bool kScored = SCORE == score::kChanged;
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row
@@ -56,7 +60,8 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     auto v_swz = [](int r) { return kD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
     constexpr int CH = (kBN * kD / 8) / NT;      // direct-to-LDS loads per thread per K (or V) tile
     static_assert(CH >= 1, "tile smaller than the workgroup");
-    static_assert(NS >= 2 && 2 * CH * (NS - 2) < 64, "too many loads in flight for vmcnt");
+    constexpr int kLoads = 2 * CH + (kScored ? 1 : 0);       // of a wave and tile
+    static_assert(NS >= 2 && kLoads * (NS - 2) < 64, "too many loads in flight for vmcnt");
 
     static_assert(sizeof(accept::Shared) <= NS * kStageB, "the ring is also what the other workgroups of a step have");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -69,6 +74,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     uint32_t* anc = (uint32_t*)(smem + NS * kStageB);        // [kMaxNodes][4]
     int32_t* spar = (int32_t*)(anc + kMaxNodes * 4);         // [kMaxNodes]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+    constexpr int kPosAt = lds_bytes_for(NS, kD), kSlopesAt = kPosAt + NS * kBN * 4;        // (changed scores)
+    int32_t* const ring_pos = (int32_t*)(smem + kPosAt);                         // [NS][kBN]
+    float* const row_slopes = (float*)(smem + kSlopesAt);                        // [WR][64]
+    float* const depths = (float*)(smem + kSlopesAt + WR * 256);                 // [kMaxNodes]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -136,7 +145,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
         }
         if constexpr (MERGE == parts::kHere || MERGE == parts::kNext)
             if (work::leaves_empty(a, team))
-                parts::finish<kD, kElem, MERGE, WR, WR>(a, team, mt, smem, [&]() __attribute__((always_inline)) { parts::put_empty<kD, 1, MERGE>(a, team, mt * WR + wave, 0); });
+                parts::finish<kD, kElem, MERGE, WR, WR>(a, team, mt, smem, [&]() __attribute__((always_inline)) { parts::put_empty<kD, 1, MERGE>(a, team, mt * WR + wave, 0); }, score::writer(sc, kShift));
         lens_end<STEP>(lens_look_back<STEP>());
         return;
     }
@@ -170,6 +179,15 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     auto stage_base = [&]() __attribute__((always_inline)) {
         return __builtin_amdgcn_readfirstlane(lds0 + ((uint32_t)issued % NS) * kStageB + wave * 1024);
     };
+    // The positions of the tile's keys, from key k0 on (changed scores; where they are not looked up something that is not used,
+    // so that the loads in flight are as many).  Every wave loads them all: each counts loads of its own.
+    auto issue_pos = [&](int k0, int last, const unsigned char* otherwise) __attribute__((always_inline)) {
+        if constexpr (kScored) {
+            const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + kPosAt + ((uint32_t)issued % NS) * (kBN * 4));
+            const unsigned char* p = otherwise ? otherwise : (const unsigned char*)(sc.key_pos + ((size_t)pw.b * a.Hkv + pw.kvh) * (size_t)a.S_cap + k0);
+            dma4(p + 4 * min(lane, last), at);
+        }
+    };
     auto issue_full = [&]() __attribute__((always_inline)) {
         const uint32_t sbase = stage_base();
         const unsigned char* kg = PAGED ? page_addr(p_key) : uniform(p_k);
@@ -179,7 +197,9 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             dma16(kg, kvo_k[c], sbase + WR * c * 1024);
             dma16(vg, kvo_v[c], sbase + WR * c * 1024 + kTileB);
         }
-        if constexpr (PAGED) p_key += kBN; else p_k += kBN * kRowB;
+        if constexpr (kScored) issue_pos(p_key, kBN - 1, sc.key_pos ? nullptr : kg);
+        if constexpr (PAGED || kScored) p_key += kBN;
+        if constexpr (!PAGED) p_k += kBN * kRowB;
     };
     auto end_tile = [&]() __attribute__((always_inline)) {
         if (pw.tile == pw.tile_end) {
@@ -211,6 +231,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
                 dma16(kg, roff + ((pc ^ k_swz(row)) << 4), sbase + WR * c * 1024);
                 dma16(vg, roff + ((pc ^ v_swz(row)) << 4), sbase + WR * c * 1024 + kTileB);
             }
+            if constexpr (kScored) issue_pos(k0, last, sc.key_pos && !tree ? nullptr : kg);
         }
         ++issued;
         end_tile();
@@ -231,8 +252,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
 #pragma unroll
         for (int c = 0; c < 32 / kRPI; ++c) dma16(qb + q_off[c], __builtin_amdgcn_readfirstlane(lds0 + q_stage + c * 1024));
     }
+    if constexpr (kScored)
+        if (sc.slopes) dma4(sc.slopes + cw.kvh * G + g, __builtin_amdgcn_readfirstlane(lds0 + kSlopesAt + wave * 256));
     for (int t = 0; t < NS - 2 && t < n_share; ++t) issue_next();
-    if (issued == NS - 2) wait_vmcnt<2 * CH * (NS - 2)>(); else wait_vmcnt<0>();
+    if (issued == NS - 2) wait_vmcnt<kLoads * (NS - 2)>(); else wait_vmcnt<0>();
 
     // ---- this lane's query row.  Q^T fragments: B operand of step t holds d = 16 t + 8 g32 + (0..7) of the row.
     // A later segment's fragments (and parent[]) are loaded before the previous one is written out.
@@ -258,6 +281,9 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     if constexpr (STEP != kNoStep) lens_read(tail, a, lens);
     while (issued < NS - 1 && issued < n_share) issue_next();
 
+    float slope = 0.f;                                    // of this lane's row, in log2 units
+    if constexpr (kScored)
+        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * kLog2e;
     int parent = -1, b_known = cw.b;
     bool masks = false;                                   // anc[] holds b_known's masks
     while (cw.b >= 0) {
@@ -277,6 +303,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
         if (!masks) {
             if (!work::tree_is_bad(a, spar)) work::build_masks(a, spar, anc);
             else if (tid < N) *(uint4*)(anc + tid * 4) = make_uint4(0, 0, 0, 0);
+            if constexpr (kScored) score::note_depth(a, anc, depths);
             __syncthreads();
             masks = true;
         }
@@ -292,6 +319,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;      // l_run: this lane's half of the keys only
+    int root = 0;                              // position of the root, where positions are looked up
+    if constexpr (kScored)
+        if (sc.key_pos) root = scalar_load_i32(uniform((const unsigned char*)sc.root_pos), (uint32_t)uniform(b) * 4u);
+    int key0 = 0;                              // the tile's first key (for changed scores)
 
     // ---- one tile: scores, (mask,) online softmax, accumulate
     // kTail: keys >= arg masked; kTree: tree tile `arg` of the unit, ancestor mask
@@ -337,6 +368,18 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);      // 8 MFMAs
         }
 
+        if constexpr (kScored) {
+#pragma unroll
+            for (int kblk = 0; kblk < 2; ++kblk) {
+                score::change(s[kblk], sc, a.scale_log2);
+                if (sc.slopes) {
+                    if constexpr (MODE == kTree) score::add_depths(s[kblk], slope, depths + arg * kBN + 32 * kblk + 4 * g32);
+                    else if (sc.key_pos) score::add_looked_up(s[kblk], slope, ring_pos + ((uint32_t)done % NS) * kBN + 32 * kblk + 4 * g32, root);
+                    else score::add_rows(s[kblk], slope, key0 + 32 * kblk + 4 * g32 - P);
+                }
+            }
+        }
+        const float to_log2 = kScored ? 1.f : a.scale_log2;
         // key of register j of block kblk, relative to the tile: 32 kblk + 8 (j/4) + 4 g32 + (j%4)
         if constexpr (MODE == kTree) {
             const int w0 = arg * 2;                     // 32-node word of block 0
@@ -369,7 +412,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             // 64 multiplications of the output accumulator are skipped.  Sum and accumulator stay
             // consistent with whatever reference is current, which is all the final division (or the
             // merge of KV splits) needs.
-            const float mt = mx * a.scale_log2;
+            const float mt = mx * to_log2;
             if (__any(mt > m_run + kLazyLog2)) {
                 const float m_new = fmaxf(m_run, mt);
                 const float alpha = fast_exp2(m_run - m_new);          // first tile: exp2(-inf) = 0
@@ -384,13 +427,13 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], a.scale_log2, kShift - m_run));
+                    const float p = fast_exp2(fmaf(s[kblk][j], to_log2, kShift - m_run));
                     s[kblk][j] = p;
                     psum += p;
                 }
             l_run += psum;
         } else {
-            const float m_new = fmaxf(m_run, mx * a.scale_log2);
+            const float m_new = fmaxf(m_run, mx * to_log2);
             float m_safe = m_new;
             if constexpr (MODE == kTree) m_safe = (m_new == -INFINITY) ? 0.f : m_new;   // row with no visible key yet
             const float alpha = fast_exp2(m_run - m_safe);
@@ -398,7 +441,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], a.scale_log2, kShift - m_safe));
+                    const float p = fast_exp2(fmaf(s[kblk][j], to_log2, kShift - m_safe));
                     s[kblk][j] = p;
                     psum += p;
                 }
@@ -459,10 +502,11 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     // vmcnt wait of its own inside the tile loop.
 #pragma unroll
     for (int t = 0; t < kKT; ++t) asm volatile("" : "+v"(qf[t]));
+    if constexpr (kScored) asm volatile("" : "+v"(slope));
 
     auto sync = [&]() __attribute__((always_inline)) {
         // tile `done` has landed once at most NS-2 younger tiles of this wave are outstanding
-        if (done + NS - 2 < n_share) wait_vmcnt<2 * CH * (NS - 2)>(); else wait_vmcnt<0>();
+        if (done + NS - 2 < n_share) wait_vmcnt<kLoads * (NS - 2)>(); else wait_vmcnt<0>();
         __syncthreads();          // every wave's part of the tile is in LDS; the stage before it is free
         if (issued < n_share) issue_next();
     };
@@ -471,10 +515,11 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     if (uniform(pw.b) == uniform(b) && uniform(pw.kvh) == uniform(kvh)) {
         const int n = uniform(p_full);
         for (int i = 0; i < n; ++i, ++done) {
-            wait_vmcnt<2 * CH * (NS - 2)>();
+            wait_vmcnt<kLoads * (NS - 2)>();
             __syncthreads();
             issue_full();
             ++issued;
+            if constexpr (kScored) key0 = (t + i) * kBN;
             if (wave_on) tile_body(std::integral_constant<int, kPlain>{}, 0);
         }
         t += n;
@@ -484,10 +529,12 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
     }
     for (const int e = min(P / kBN, t_end); t < e; ++t, ++done) {
         sync();
+        if constexpr (kScored) key0 = t * kBN;
         if (wave_on) tile_body(std::integral_constant<int, kPlain>{}, 0);
     }
     for (const int e = min(u_pref, t_end); t < e; ++t, ++done) {
         sync();
+        if constexpr (kScored) key0 = t * kBN;
         if (wave_on) tile_body(std::integral_constant<int, kTail>{}, P - t * kBN);
     }
     for (; t < t_end; ++t, ++done) {
@@ -501,6 +548,8 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
         if (nw.b >= 0) {
             if (nw.b != b && tid < N) parent = a.parent[(size_t)nw.b * N + tid];
             load_q(nw.b, nw.kvh);
+            if constexpr (kScored)
+                if (sc.slopes) slope = sc.slopes[nw.kvh * G + g] * kLog2e;
         }
         if (mt == 0 && tid == 0) work::note_parts(a, team, cw);
     }
@@ -521,12 +570,13 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
             parts::put<kD, 1, MERGE, true>(Arguments().attn(), team, mt * WR + wave, 0, m_run, l_tot, [&](int q) __attribute__((always_inline)) {
                 return f32x4{o[q >> 2][4 * (q & 3)], o[q >> 2][4 * (q & 3) + 1], o[q >> 2][4 * (q & 3) + 2], o[q >> 2][4 * (q & 3) + 3]};
             });
-        });
+        }, score::writer(sc, kShift));
         lens_end<STEP>(left);
         return;
     }
     if (MERGE == parts::kWhole || work::walk_is_whole(a, cw)) {
         if (rvalid) {
+        if (g32 == 0) score::writer(sc, kShift)(((size_t)b * N + node) * a.Hq + kvh * G + g, m_run, l_tot);
         const float inv = (l_tot > 0.f) ? 1.f / l_tot : 0.f;
         bf16_t* orow = (bf16_t*)a.out + (((size_t)b * N + node) * a.Hq + kvh * G + g) * kD + 4 * g32;
 #pragma unroll
@@ -563,15 +613,16 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail) {
 
 int pick_wr(int M) { return M <= 128 ? 4 : 8; }
 
-template <int WR, int NS, int WPE, bool PAGED, bool F16, int D, StepKind STEP, parts::Merge MERGE>
-hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st) {
-    constexpr int kLds = lds_bytes_for(NS, D);
+template <int WR, int NS, int WPE, bool PAGED, bool F16, int D, StepKind STEP, parts::Merge MERGE, score::Kind SCORE = score::kPlain>
+hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st, const score::Args<SCORE>& sc = {}) {
+    constexpr int kLds = SCORE == score::kPlain ? lds_bytes_for(NS, D) : scored_lds_bytes_for(NS, D, WR);
+    static_assert((WR == 4 && D == 64 ? 2 : 1) * kLds <= 160 * 1024, "LDS of a CU");
     static std::atomic<uint64_t> lds_set{0};
-    const hipError_t ea = ensure_dynamic_lds((const void*)tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE>, kLds, lds_set);
+    const hipError_t ea = ensure_dynamic_lds((const void*)tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE, SCORE>, kLds, lds_set);
     if (ea != hipSuccess) return ea;
     a.attn_wgs = attn_workgroups(a);
     const dim3 grid = launch_grid(a, rest_of(a, tail)), block(WR * 64);
-    hipLaunchKernelGGL((tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE>), grid, block, kLds, st, a, tail);
+    hipLaunchKernelGGL((tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE, SCORE>), grid, block, kLds, st, a, tail, sc);
     return hipGetLastError();
 }
 
@@ -589,6 +640,24 @@ hipError_t launch_rows(const AttnArgs& a, const StepTail<STEP>& tail, hipStream_
     if constexpr (!PAGED && STEP == kNoStep)
         if (a.tag == 0) return launch_rows<PAGED, F16, D, STEP, parts::kNext>(a, tail, st);
     return launch_rows<PAGED, F16, D, STEP, parts::kHere>(a, tail, st);
+}
+// ... of attention with changed scores
+template <bool PAGED, bool F16, int D, parts::Merge MERGE>
+hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+    const StepTail<kNoStep> none;
+    return pick_wr(a.M) == 4 ? launch<4, 4, D == 64 ? 2 : 1, PAGED, F16, D, kNoStep, MERGE, score::kChanged>(a, none, st, sc)
+                             : launch<8, 4, 2, PAGED, F16, D, kNoStep, MERGE, score::kChanged>(a, none, st, sc);
+}
+template <bool PAGED, bool F16, int D>
+hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+    return a.split == 1   ? launch_scored<PAGED, F16, D, parts::kWhole>(a, sc, st)
+           : a.split == 0 ? launch_scored<PAGED, F16, D, parts::kShares>(a, sc, st)
+                          : launch_scored<PAGED, F16, D, parts::kHere>(a, sc, st);
+}
+template <bool F16>
+hipError_t launch_large_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+    if (a.D == 64) return a.block_table ? launch_scored<true, F16, 64>(a, sc, st) : launch_scored<false, F16, 64>(a, sc, st);
+    return a.block_table ? launch_scored<true, F16, 128>(a, sc, st) : launch_scored<false, F16, 128>(a, sc, st);
 }
 template <bool F16, int D>
 hipError_t launch_as(const AttnArgs& a, const StepTail<kGreedyStep>* step, hipStream_t st) {

@@ -16,6 +16,7 @@
 //                P^T is used straight out of the score accumulator: register j of lane half g holds key
 //                8 (j/4) + 4 g + j%4, so step j multiplies V rows that far apart.
 #pragma once
+#include "attn_score.h"
 #include "attn_step.h"
 
 namespace s4c {
@@ -62,7 +63,11 @@ struct Cfg {
     static_assert(sizeof(accept::Shared) <= kRingB, "the ring is also what the other workgroups of a step have");
     static constexpr int kPerCu = 2 * kLdsBytes <= 160 * 1024 ? 2 : 1;
     static_assert(kLdsBytes <= 160 * 1024, "LDS of one CU");
-    static_assert(kCH >= 1 && 2 * kCH * (kNR - 1) < 64, "loads in flight are counted in vmcnt");
+    // with changed scores behind it: positions of the ring's keys, slopes of every wave's rows, depths of the nodes
+    static constexpr int kPosB = kNR * kKG * kBN * 4, kSlopeB = kWaves * 256;
+    static constexpr int kScoredLdsBytes = kLdsBytes + kPosB + kSlopeB + kMaxNodes * 4;
+    static_assert(kPerCu * kScoredLdsBytes <= 160 * 1024, "as many workgroups on a CU as without");
+    static_assert(kCH >= 1 && (2 * kCH + 1) * (kNR - 1) < 64, "loads in flight are counted in vmcnt");
     // 16-byte chunk swizzle of row r: K is read as one chunk of 16 (or 32) consecutive rows at a time, V as 4 rows x
     // 64 bytes (16-bit) or two rows 4 apart x 128 bytes (fp32); both spread over all banks
     static __device__ __forceinline__ int k_swz(int r) {
@@ -76,9 +81,10 @@ struct Cfg {
     }
 };
 
-template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE>
+template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kPerCu * C::kWaves / 4, 2)))
-void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
+void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
+    constexpr bool kScored = SCORE == score::kChanged;
     constexpr int kD = C::kD, kKG = C::kKG, kRBW = C::kRBW, kNR = C::kNR, kRowB = C::kRowB;
     constexpr int kThreads = C::kThreads, kCH = C::kCH;
     constexpr bool kIs32 = C::kElem == kF32, F16 = C::kElem == kH16;
@@ -88,6 +94,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
     constexpr float kLag = kLagLog2<!kIs32 && kParts == 1>;
     constexpr int kLPR = kRowB / 16;                          // lanes (16-byte chunks) per row in a direct-to-LDS load
     constexpr int kRPI = 64 / kLPR;                           // rows per load instruction
+    constexpr int kLoads = 2 * kCH + (kScored ? 1 : 0);       // of a wave and round
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     if constexpr (STEP != kNoStep)
         if (__builtin_expect(blockIdx.y > 0, 0)) {          // (the attention's code first: a far jump at its start costs a fetch)
@@ -97,6 +104,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
     uint32_t* anc = (uint32_t*)(smem + C::kRingB);            // [kMaxNodes][4]
     int32_t* spar = (int32_t*)(anc + kMaxNodes * 4);          // [kMaxNodes]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+    int32_t* const ring_pos = (int32_t*)(smem + C::kLdsBytes);                   // (changed scores) [kNR][kKG][kBN]
+    float* const row_slopes = (float*)(smem + C::kLdsBytes + C::kPosB);          // [waves][64]
+    float* const depths = (float*)(smem + C::kLdsBytes + C::kPosB + C::kSlopeB); // [kMaxNodes]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -174,7 +184,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             if (work::leaves_empty(a, team))
                 parts::finish<kD, C::kElem, MERGE, C::kWaves, kRBW>(a, team, mt, smem, [&]() __attribute__((always_inline)) {
                     if (kg < kOwners) parts::put_empty<kD, kOwners, MERGE>(a, team, mt * kRBW + rb, kg);
-                });
+                }, score::writer(sc, kShift));
         lens_end<STEP>(lens_look_back<STEP>());
         return;
     }
@@ -208,6 +218,15 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
     auto stage_base = [&]() __attribute__((always_inline)) {
         return __builtin_amdgcn_readfirstlane(lds0 + ((uint32_t)issued % kNR) * C::kRoundB + kg * C::kTileB + rb * kCH * 1024);
     };
+    // The positions of the round's keys, from key k0 on (changed scores; where they are not looked up something that is not used,
+    // so that the loads in flight are as many).
+    auto issue_pos = [&](int k0, int last, const unsigned char* otherwise) __attribute__((always_inline)) {
+        if constexpr (kScored) {
+            const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + C::kLdsBytes + (((uint32_t)issued % kNR) * kKG + kg) * (kBN * 4));
+            const unsigned char* p = otherwise ? otherwise : (const unsigned char*)(sc.key_pos + ((size_t)pw.b * a.Hkv + pw.kvh) * (size_t)a.S_cap + k0);
+            if (lane < kBN) dma4(p + 4 * min(lane, last), at);
+        }
+    };
     auto issue_full = [&]() __attribute__((always_inline)) {
         const uint32_t sbase = stage_base();
         const unsigned char* kgp = PAGED ? page_addr(p_key) : uniform(p_k);
@@ -217,7 +236,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             dma16(kgp, kvo_k[c], sbase + c * 1024);
             dma16(vgp, kvo_v[c], sbase + c * 1024 + C::kTileKB);
         }
-        if constexpr (PAGED) p_key += kKG * kBN; else p_k += kKG * kBN * kRowB;
+        if constexpr (kScored) issue_pos(p_key, kBN - 1, sc.key_pos ? nullptr : kgp);
+        if constexpr (PAGED || kScored) p_key += kKG * kBN;
+        if constexpr (!PAGED) p_k += kKG * kBN * kRowB;
     };
     auto end_round = [&]() __attribute__((always_inline)) {
         if (pw.tile >= pw.tile_end) {
@@ -249,6 +270,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
                 dma16(kgp, roff + ((pc ^ C::k_swz(row)) << 4), sbase + c * 1024);
                 dma16(vgp, roff + ((pc ^ C::v_swz(row)) << 4), sbase + c * 1024 + C::kTileKB);
             }
+            if constexpr (kScored) issue_pos(k0, last, sc.key_pos && !tree ? nullptr : kgp);
         }
         ++issued;
         pw.tile += kKG;
@@ -269,6 +291,8 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
 #pragma unroll
         for (int c = 0; c < C::kTileKB / 1024; ++c) dma16(qb + q_off[c], __builtin_amdgcn_readfirstlane(lds0 + q_stage + c * 1024));
     }
+    if constexpr (kScored)
+        if (sc.slopes) dma4(sc.slopes + cw.kvh * G + gh, __builtin_amdgcn_readfirstlane(lds0 + C::kLdsBytes + C::kPosB + wave * 256));
 #pragma unroll
     for (int r = 0; r < kNR - 1; ++r)
         if (pw.b >= 0) issue_round();
@@ -276,7 +300,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
         __syncthreads();
         lens_read(tail, a, lens);
     }
-    if (issued == kNR - 1) wait_vmcnt<2 * kCH * (kNR - 1)>(); else wait_vmcnt<0>();
+    if (issued == kNR - 1) wait_vmcnt<kLoads * (kNR - 1)>(); else wait_vmcnt<0>();
 
     // ---- this lane's query row; a later segment's Q fragments (and parent[]) are loaded before the previous one is
     // written out
@@ -294,6 +318,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             if (rvalid) qf[t] = *(const uint4*)(qrow + 32 * t);
         }
     };
+    float slope = 0.f;                                        // of this lane's row, in log2 units
+    if constexpr (kScored)
+        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * kLog2e;
     int parent = -1, b_known = cw.b;
     bool masks = false;                                       // anc[] holds b_known's masks
     while (cw.b >= 0) {
@@ -316,6 +343,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
                 __syncthreads();                              // (the first segment: parent[] has landed)
                 if (!work::tree_is_bad(a, spar)) work::build_masks(a, spar, anc);
                 else if (tid < N) *(uint4*)(anc + tid * 4) = make_uint4(0, 0, 0, 0);
+                if constexpr (kScored) score::note_depth(a, anc, depths);
                 __syncthreads();
                 masks = true;
             }
@@ -331,10 +359,14 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
         float m_run = -INFINITY, l_run = 0.f;
+        int root = 0;                                         // position of the root, where positions are looked up
+        if constexpr (kScored)
+            if (sc.key_pos) root = scalar_load_i32(uniform((const unsigned char*)sc.root_pos), (uint32_t)uniform(b) * 4u);
 
         // one 32-key tile: S^T = K Q^T, (mask,) online softmax, O^T += V^T P^T
         // masked: bit 8 (j/4) + j%4 of `visible` tells whether register j's key counts for this lane's row
-        auto tile = [&](auto masked_tag, uint32_t visible) __attribute__((always_inline)) {
+        // my: the tile's number in the unit (for changed scores)
+        auto tile = [&](auto masked_tag, uint32_t visible, int my) __attribute__((always_inline)) {
             constexpr bool MASKED = decltype(masked_tag)::value;
             const lds_u8* stage = (const lds_u8*)smem + ((uint32_t)done % kNR) * C::kRoundB + kg * C::kTileB;
             f32x16 s;
@@ -369,6 +401,16 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s[j] += s1[j];
             }
+            constexpr bool kLog2Units = kScored;              // of s from here on
+            if constexpr (kScored) {
+                score::change(s, sc, a.scale_log2);
+                if (sc.slopes) {
+                    if (MASKED && my >= u_pref) score::add_depths(s, slope, depths + (my - u_pref) * kBN + 4 * g32);
+                    else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);
+                    else score::add_rows(s, slope, my * kBN + 4 * g32 - P);
+                }
+            }
+            const float to_log2 = kLog2Units ? 1.f : a.scale_log2;
             if constexpr (MASKED) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
@@ -377,7 +419,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             float mx = s[0];
 #pragma unroll
             for (int j = 1; j < 16; j += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[j]), s[(j + 1) & 15]);
-            mx = max_across_halves(mx) * a.scale_log2;
+            mx = max_across_halves(mx) * to_log2;
             // The reference moves only when some row of the wave outgrew it by more than 2^kLag (always at its first
             // visible key); until then the accumulator is not touched.
             if (__any(mx > m_run + kLag)) {
@@ -396,7 +438,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             float psum = 0.f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float p = fast_exp2(fmaf(s[j], a.scale_log2, kShift - m_ref));
+                const float p = fast_exp2(fmaf(s[j], to_log2, kShift - m_ref));
                 s[j] = p;
                 psum += p;
             }
@@ -440,16 +482,17 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
         // inside the round loop (which would also wait for the rounds just issued).
 #pragma unroll
         for (int t = 0; t < kKT; ++t) asm volatile("" : "+v"(qf[t].x), "+v"(qf[t].y), "+v"(qf[t].z), "+v"(qf[t].w));
+        if constexpr (kScored) asm volatile("" : "+v"(slope));
         auto sync_and_prefetch = [&]() __attribute__((always_inline)) {
             // this wave's share of round `done` has landed once at most NR - 2 younger rounds are outstanding
-            if (kNR > 2 && issued - done == kNR - 1) wait_vmcnt<2 * kCH * (kNR - 2)>(); else wait_vmcnt<0>();
+            if (kNR > 2 && issued - done == kNR - 1) wait_vmcnt<kLoads * (kNR - 2)>(); else wait_vmcnt<0>();
             __syncthreads();           // everybody's has; the round before it is no longer read
             if (pw.b >= 0) issue_round();
         };
         int t = uniform(cw.tile);
         for (const int e = min(P / kBN, t_end) - kKG; t <= e; t += kKG, ++done) {
             sync_and_prefetch();
-            tile(std::integral_constant<bool, false>{}, 0u);
+            tile(std::integral_constant<bool, false>{}, 0u, t + kg);
         }
         for (; t < t_end; t += kKG, ++done) {
             sync_and_prefetch();
@@ -463,7 +506,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
                 const int nvalid = P - my * kBN;                         // the ragged last prefix tile: 1 .. 31 keys
                 visible = (nvalid >= kBN ? 0xFFFFFFFFu : (1u << nvalid) - 1u) >> (4 * g32);
             }
-            tile(std::integral_constant<bool, true>{}, visible);
+            tile(std::integral_constant<bool, true>{}, visible, my);
         }
 
         work::Walk nw = cw;
@@ -472,6 +515,8 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
             if (nw.b >= 0) {
                 if (nw.b != b && tid < N) parent = a.parent[(size_t)nw.b * N + tid];
                 load_q(nw.b, nw.kvh);
+                if constexpr (kScored)
+                    if (sc.slopes) slope = sc.slopes[nw.kvh * G + gh] * kLog2e;
             }
         }
         const int flagged = (work::tree_is_bad(a, spar) ? S4C_SEQ_BAD_TREE : 0) | (len_bad ? S4C_SEQ_BAD_LEN : 0);
@@ -564,13 +609,14 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
         if constexpr (MERGE == parts::kHere || MERGE == parts::kNext) {
             parts::finish<kD, C::kElem, MERGE, C::kWaves, kRBW>(a, team, mt, smem, [&]() __attribute__((always_inline)) {
                 if (kg < kOwners) parts::put<kD, kOwners, MERGE>(a, team, mt * kRBW + rb, kg, m_max, l_tot, piece);
-            });
+            }, score::writer(sc, kShift));
             lens_end<STEP>(left);
             return;
         }
         if (MERGE == parts::kWhole || work::walk_is_whole(a, cw)) {
             const float inv = (l_tot > 0.f) ? 1.f / l_tot : 0.f;
             const size_t o0 = (((size_t)b * a.N + node) * a.Hq + kvh * G + gh) * kD + 32 * kOwn * kg + 4 * g32;
+            if (rvalid && kg == 0 && g32 == 0) score::writer(sc, kShift)(((size_t)b * a.N + node) * a.Hq + kvh * G + gh, m_max, l_tot);
             if (rvalid && kg < kOwners)
 #pragma unroll
                 for (int q = 0; q < 4 * kOwn; ++q) parts::store_out<C::kElem>(a.out, o0 + 8 * q, piece(q) * inv);
@@ -587,14 +633,15 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail) {
     }
 }
 
-template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE>
-hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st) {
+template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE, score::Kind SCORE = score::kPlain>
+hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st, const score::Args<SCORE>& sc = {}) {
+    constexpr int kLds = SCORE == score::kPlain ? C::kLdsBytes : C::kScoredLdsBytes;
     static std::atomic<uint64_t> lds_set{0};
-    const hipError_t ea = ensure_dynamic_lds((const void*)tree_attn_smallm_kernel<C, PAGED, STEP, MERGE>, C::kLdsBytes, lds_set);
+    const hipError_t ea = ensure_dynamic_lds((const void*)tree_attn_smallm_kernel<C, PAGED, STEP, MERGE, SCORE>, kLds, lds_set);
     if (ea != hipSuccess) return ea;
     a.attn_wgs = attn_workgroups(a);
     const dim3 grid = launch_grid(a, rest_of(a, tail)), block(C::kThreads);
-    hipLaunchKernelGGL((tree_attn_smallm_kernel<C, PAGED, STEP, MERGE>), grid, block, C::kLdsBytes, st, a, tail);
+    hipLaunchKernelGGL((tree_attn_smallm_kernel<C, PAGED, STEP, MERGE, SCORE>), grid, block, kLds, st, a, tail, sc);
     return hipGetLastError();
 }
 template <class C, bool PAGED, StepKind STEP>
@@ -619,6 +666,21 @@ auto with_cfg(int D, int rows, Use use) {
         if (D == 64) return rows == 32 ? use(Cfg<E, 64, 4, 1, 2>{}) : use(Cfg<E, 64, 2, 2, 4>{});
         return rows == 32 ? use(Cfg<E, 128, 4, 1, 2>{}) : use(Cfg<E, 128, 2, 2, 2>{});
     }
+}
+// ... of attention with changed scores
+template <class C, bool PAGED>
+hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+    const StepTail<kNoStep> none;
+    if (a.split == 1) return launch<C, PAGED, kNoStep, parts::kWhole, score::kChanged>(a, none, st, sc);
+    if (a.split == 0) return launch<C, PAGED, kNoStep, parts::kShares, score::kChanged>(a, none, st, sc);
+    return launch<C, PAGED, kNoStep, parts::kHere, score::kChanged>(a, none, st, sc);
+}
+template <Elem E>
+hipError_t launch_smallm_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+    return with_cfg<E>(a.D, a.tile_rows, [&](auto c) {
+        typedef decltype(c) C;
+        return a.block_table ? launch_scored<C, true>(a, sc, st) : launch_scored<C, false>(a, sc, st);
+    });
 }
 // A launch for one element type; instantiated in a translation unit of its own each (they take a minute to compile).
 template <Elem E>

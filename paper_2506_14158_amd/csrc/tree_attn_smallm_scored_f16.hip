@@ -1,0 +1,8 @@
+// tree_attn_smallm.h with changed scores, for fp16 data.
+#include "tree_attn_smallm.h"
+
+namespace s4c {
+
+hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) { return launch_smallm_scored<kH16>(a, sc, st); }
+
+}  // namespace s4c

@@ -753,16 +753,22 @@ s4c_status s4c_verify_step(const s4c_step* p, void* hip_stream) {
 // ---- changed scores, and a cache that rows are evicted from
 namespace {
 
+// (by its bits: this file is compiled without regard for NaN)
+bool is_finite(float x) {
+    uint32_t u;
+    __builtin_memcpy(&u, &x, 4);
+    return (u & 0x7F800000u) != 0x7F800000u;
+}
 // How the scores of a call with this scale are changed; false: not a score that the kernels take.
 bool score_args(const s4c_score* sc, float scale, int32_t D, score::Args<score::kChanged>* a, s4c_status* why) {
     *a = {};
     if (!sc) return true;
     if (sc->key_pos && !sc->root_pos) { *why = S4C_ERR_NULL; return false; }
-    if (!(sc->cap >= 0.f)) { *why = S4C_ERR_SHAPE; return false; }
+    if (!is_finite(sc->cap) || sc->cap < 0.f) { *why = S4C_ERR_SHAPE; return false; }
     if (sc->cap > 0.f) {
         a->cap_log2 = sc->cap * kLog2e;
         a->to_y = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) / sc->cap;
-        if (!isfinite(2.f * a->cap_log2) || !isfinite(a->to_y) || a->cap_log2 <= 0.f) { *why = S4C_ERR_SHAPE; return false; }
+        if (!is_finite(2.f * a->cap_log2) || !is_finite(a->to_y)) { *why = S4C_ERR_SHAPE; return false; }
     }
     a->slopes = sc->slopes;
     a->key_pos = sc->key_pos;

@@ -10,10 +10,13 @@ from . import binding as _b
 
 class TreeVerifier:
     """Pre-allocates outputs and workspaces for one shape and enqueues
-    s4c_tree_attn -> s4c_accept_path -> s4c_kv_compact on the current stream."""
+    s4c_tree_attn -> s4c_accept_path -> s4c_kv_compact on the current stream.
+
+    For a cache that is kept to ``budget`` rows: step with a Score (its lse is kept), kv_weigh for every layer, root_pos advanced by
+    accept_len + 1, and kv_evict over all layers whenever the cache has grown far enough beyond the budget."""
 
     def __init__(self, B, N, Hq, Hkv, D, S_cap, V, dtype: torch.dtype, max_path: int, max_cache_len: int,
-                 device="cuda"):
+                 device="cuda", layers: int = 1, budget: int = 0, recent: int = 0):
         self.B, self.N, self.Hq, self.Hkv, self.D, self.S_cap, self.V = B, N, Hq, Hkv, D, S_cap, V
         self.dtype, self.max_path, self.max_cache_len = dtype, max_path, max_cache_len
         code = {torch.float32: _b.S4C_F32, torch.bfloat16: _b.S4C_BF16, torch.float16: _b.S4C_F16}[dtype]
@@ -35,11 +38,36 @@ class TreeVerifier:
         # sequential acceptance: the exchange slots of the workgroup teams (a few hundred KB at most), allocated
         # here so that no call allocates later (a step may be under graph capture)
         self.resample_ws = _b.alloc_workspace(max(256, _b.s4c_accept_resample_workspace_size(B, N, V, max_path)), device)
+        # the log-sum-exp of the last attention with changed scores; eviction
+        self.lse = torch.empty(B, N, Hq, dtype=torch.float32, device=device)
+        self.weigh_status = torch.zeros(B, **i32)
+        self.layers, self.budget, self.recent = layers, budget, recent
+        if budget > 0:
+            self.kept = torch.empty(layers, B, Hkv, budget, **i32)
+            self.evict_status = torch.zeros(B, **i32)
+            self.evict_ws = _b.alloc_workspace(_b.s4c_kv_evict_workspace_size(layers, B, Hkv, budget, S_cap), device)
         self.num_splits = _b.s4c_tree_attn_num_splits(self.shape, max_cache_len)
 
     def tree_attn(self, q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, scale: float = 0.0):
         return _b.s4c_tree_attn(q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, self.max_cache_len,
                                 self.out, scale, self.attn_status, self.attn_ws)
+
+    def tree_attn_scored(self, q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, score: _b.Score, scale: float = 0.0, out=None, lse=None):
+        """Attention with changed scores; the output and log-sum-exp go to self.out and self.lse unless others are given."""
+        return _b.s4c_tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, self.max_cache_len, score,
+                                       self.out if out is None else out, self.lse if lse is None else lse, scale, self.attn_status,
+                                       self.attn_ws)
+
+    def kv_weigh(self, q, k_cache, cache_len, score: _b.Score, weight, scale: float = 0.0, lse=None):
+        """After the path's rows were appended: what its rows attended to is added to ``weight`` [B][Hkv][S_cap], and their positions are
+        written into score.key_pos."""
+        _b.s4c_kv_weigh(q, k_cache, self.lse if lse is None else lse, cache_len, self.path, self.accept_len, self.S_cap, score, weight, weight,
+                        scale, self.weigh_status)
+
+    def kv_evict(self, k_cache, v_cache, weight, key_pos, cache_len, next_pos):
+        """Every layer's cache [layers][B][Hkv][S_cap][D] down to self.budget rows, with its totals and positions, all in place."""
+        _b.s4c_kv_evict(k_cache, v_cache, weight, key_pos, cache_len, next_pos, self.budget, self.recent, weight, key_pos, cache_len,
+                        self.evict_ws, self.kept, self.evict_status)
 
     def accept_path(self, logits, parent, tokens, mode: int, p_draft=None, uniforms=None, temperature=1.0):
         _b.s4c_accept_path(logits, parent, tokens, mode, self.max_path, self.path, self.accept_len,
@@ -62,7 +90,12 @@ class TreeVerifier:
                            features_out, self.dst_index, self.compact_status)
 
     def step(self, q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, logits, tokens, mode: int,
-             p_draft=None, uniforms=None, temperature: float = 1.0, scale: float = 0.0):
+             p_draft=None, uniforms=None, temperature: float = 1.0, scale: float = 0.0, score: Optional[_b.Score] = None):
+        if score is not None:
+            self.tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, score, scale)
+            self.accept_path(logits, parent, tokens, mode, p_draft, uniforms, temperature)
+            self.kv_compact(k_tree, v_tree, k_cache, v_cache, cache_len)
+            return
         if _b.s4c_verify_step(q, k_tree, v_tree, k_cache, v_cache, cache_len, parent, logits, tokens, mode, p_draft, uniforms,
                               temperature, scale, self.out, self.attn_status, self.attn_ws, self.path, self.accept_len,
                               self.accepted_tokens, self.bonus_token, self.accept_status, self.accept_ws, self.dst_index,

@@ -1,0 +1,513 @@
+"""Attention weights of cache rows, eviction, and a conversation over a bounded cache, against the 64-bit definitions."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as K
+from paper_2506_14158_amd import binding as B
+from paper_2506_14158_amd.verify import TreeVerifier
+from tests.test_gpu_scored import CODE, DT, f64
+
+pytestmark = pytest.mark.gpu
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+def host(t):
+    return None if t is None else t.cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ weights
+class Weigh:
+    def __init__(self, seed, B_, N, Hq, Hkv, D, dtype, lengths, accepted, S_cap, page=0, max_path=None, node=None):
+        g = torch.Generator().manual_seed(seed)
+        r = np.random.default_rng(seed)
+        f = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(DT[dtype]).cuda()
+        self.dtype, self.page, self.D, self.G, self.S_cap = dtype, page, D, Hq // Hkv, S_cap
+        self.q = f(B_, N, Hq, D, std=2.0)
+        self.table = None
+        if page:
+            blocks = S_cap // page
+            self.kc = f(B_ * blocks + 1, Hkv, page, D)
+            self.table = torch.from_numpy(r.permutation(B_ * blocks + 1)[:B_ * blocks].reshape(B_, blocks).astype(np.int32)).cuda()
+        else:
+            self.kc = f(B_, Hkv, S_cap, D)
+        max_path = max_path or max(accepted) + 1
+        path = np.full((B_, max_path), -1, dtype=np.int32)
+        for b, L in enumerate(accepted):
+            path[b, :L + 1] = node if node is not None else np.concatenate([[0], 1 + np.sort(r.permutation(N - 1)[:L])])
+        self.path = torch.from_numpy(path).cuda()
+        self.acc = torch.tensor(accepted, **I32)
+        self.len = torch.tensor(lengths, **I32)
+        self.slopes = torch.tensor([2.0 ** (-6.0 * (h + 1) / Hq) for h in range(Hq)], dtype=torch.float32, device="cuda")
+        self.pos = torch.from_numpy(np.stack([[r.permutation(3 * S_cap)[:S_cap] for _ in range(Hkv)] for _ in range(B_)]).astype(np.int32)).cuda()
+        self.root = torch.full((B_,), 3 * S_cap, **I32)
+        self.win = torch.rand(B_, Hkv, S_cap, generator=g).cuda()
+        self.w = torch.full_like(self.win, 7.0)
+        self.status = torch.full((B_,), 9, **I32)
+        # what an attention before it could have left: near the largest score, so that weights are neither 0 nor huge
+        self.lse = (torch.randn(B_, N, Hq, generator=g) * 2.0 + 5.0).cuda()
+
+    def score(self, cap, bias):
+        return B.Score(cap, self.slopes if bias != "none" else None, *((self.pos, self.root) if bias == "kept" else (None, None)))
+
+    def call(self, score, in_place=False, m=None, scale=0.0):
+        out = self.win if in_place else self.w
+        m = self.S_cap if m is None else m
+        if self.page:
+            B.s4c_kv_weigh_paged(self.q, self.kc, self.table, self.lse, self.len, self.path, self.acc, m, score, self.win, out, scale, self.status)
+        else:
+            B.s4c_kv_weigh(self.q, self.kc, self.lse, self.len, self.path, self.acc, m, score, self.win, out, scale, self.status)
+        torch.cuda.synchronize()
+
+    def want(self, score, scale=0.0):
+        kc = f64(self.kc) if not self.page else K.gather_pages(f64(self.kc), host(self.table))
+        return K.kv_weigh(f64(self.q), kc, f64(self.lse), host(self.len), host(self.path), host(self.acc), f64(self.win), scale, score.cap,
+                          None if score.slopes is None else f64(score.slopes), host(score.key_pos), host(score.root_pos))
+
+    def check(self, score, want, got, before):
+        """A weight is exp of a difference: its score is off as in the attention (D fp32 additions of sum |q k|, which is below 2 D here; 12
+        roundings of its size; 2^-22 of the cap), the log-sum-exp is rounded in log2 units, and a row's R terms are added up in fp32, then
+        to the total."""
+        weight, pos, added = want
+        L = int(self.acc.max())
+        size = np.abs(f64(self.lse)).max() + 20 + score.cap
+        if score.slopes is not None:             # keys whose weight counts (> 2^-30) are biased by less than what is left of 20 + ...
+            size += 40.0
+        x = 2.0 ** -24 * (self.D * 2 * self.D * (1 / np.sqrt(self.D)) + 14 * size + 6 * score.cap)
+        tol = added * (np.exp(x) - 1 + 2.0 ** -24 * ((L + 1) * self.G + 8)) + 2.0 ** -23 * np.abs(weight) + 1e-12
+        for b, n in enumerate(host(self.len)):
+            err = np.abs(f64(got)[b, :, :n] - weight[b, :, :n])
+            # a total beyond fp32's largest number is +infinity (these lse come from no attention: a slope of 0.77 over 127 rows alone
+            # makes weights of e^98 = 3e42)
+            err[np.isposinf(f64(got)[b, :, :n]) & ((weight + tol)[b, :, :n] > np.finfo(np.float32).max)] = 0.0
+            assert (err <= tol[b, :, :n]).all(), (b, err.max(), (err / tol[b, :, :n]).max())
+            assert torch.equal(got[b, :, n:], before[b, :, n:])
+        if pos is not None:
+            assert np.array_equal(host(score.key_pos), pos)
+
+
+WEIGH = {
+    # name: B, N, Hq, Hkv, D, lengths, accepted, S_cap, page
+    "the first token": (2, 1, 4, 4, 64, (1, 1), (0, 0), 16, 0),
+    "one token": (3, 1, 8, 2, 128, (33, 64, 65), (0, 0, 0), 80, 0),
+    "a path, ragged": (3, 20, 8, 4, 128, (300, 17, 1029), (4, 0, 7), 1040, 0),
+    "all rows are the path's": (1, 40, 4, 2, 64, (40,), (39,), 40, 0),
+    "odd group": (2, 9, 15, 3, 64, (200, 255), (3, 8), 257, 0),
+    "128 rows and one more": (1, 43, 9, 3, 128, (333,), (42,), 334, 0),
+    "several turns of the query rows": (2, 128, 16, 4, 64, (520, 130), (127, 99), 528, 0),
+    "paged": (3, 12, 8, 2, 128, (129, 64, 256), (5, 2, 0), 256, 64),
+    "paged, large pages": (2, 128, 8, 4, 64, (700, 128), (60, 127), 1024, 512),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("name", WEIGH)
+def test_weights_against_the_definition(name, dtype):
+    c = Weigh(sum(map(ord, name)), *WEIGH[name][:5], dtype, *WEIGH[name][5:])
+    for cap, bias in ((0.0, "none"), (3.0, "none"), (20.0, "rows"), (0.0, "rows"), (10.0, "kept")):
+        s = c.score(cap, bias)
+        want = c.want(s)
+        before = c.w.fill_(7.0).clone()
+        c.call(s)
+        assert not c.status.any()
+        c.check(s, want, c.w, before)
+    # in place: the same bits
+    before = c.win.clone()
+    c.call(s, in_place=True)
+    for b, n in enumerate(host(c.len)):
+        assert torch.equal(c.win[b, :, :n], c.w[b, :, :n]) and torch.equal(c.win[b, :, n:], before[b, :, n:])
+
+
+def test_weights_with_a_node_named_twice_and_a_scale():
+    """The path is what it says, whatever nodes it names; `scale` is the caller's."""
+    c = Weigh(3, 2, 7, 4, 2, 64, "bf16", (90, 77), (3, 3), 96, node=[0, 5, 5, 2])
+    s = c.score(0.0, "none")
+    want = c.want(s, 0.05)
+    before = c.w.clone()
+    c.call(s, scale=0.05)
+    c.check(s, want, c.w, before)
+
+
+def test_weights_of_an_attention():
+    """Attention, the path appended, weights: every query row gives away a weight of one."""
+    Bn, N, Hq, Hkv, D, S_cap = 2, 24, 8, 2, 128, 640
+    g = torch.Generator().manual_seed(1)
+    f = lambda *s: torch.randn(*s, generator=g).to(torch.bfloat16).cuda()
+    q, kt, vt, kc, vc = f(Bn, N, Hq, D), f(Bn, N, Hkv, D), f(Bn, N, Hkv, D), f(Bn, Hkv, S_cap, D), f(Bn, Hkv, S_cap, D)
+    v = TreeVerifier(Bn, N, Hq, Hkv, D, S_cap, 100, torch.bfloat16, N, S_cap)
+    parent = torch.tensor([[-1] + list(range(N - 1))] * Bn, **I32)
+    n = torch.tensor([500, 77], **I32)
+    slopes = torch.tensor([2.0 ** -(h + 1) for h in range(Hq)], device="cuda")
+    s = B.Score(15.0, slopes)
+    v.tree_attn_scored(q, kt, vt, kc, vc, n, parent, s)
+    v.path.copy_(torch.arange(N, **I32).expand(Bn, N))
+    v.accept_len.copy_(torch.tensor([N - 1, 10], **I32))
+    v.kv_compact(kt, vt, kc, vc, n)
+    w = torch.zeros(Bn, Hkv, S_cap, device="cuda")
+    v.kv_weigh(q, kc, n, s, w)
+    assert n.tolist() == [500 + N, 88] and not v.weigh_status.any()
+    total = f64(w).sum(-1)
+    assert np.abs(total / (Hq // Hkv * np.array([[N], [11]])) - 1).max() < 1e-4      # (scores of the two calls differ in their last bits)
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_weights_of_flagged_sequences(page):
+    """Not valid: nothing is written.  A sequence that the attention flagged (lse +infinity) gives no weight."""
+    c = Weigh(4, 6, 9, 4, 2, 64, "bf16", (64, 60, 50, 40, 128, 100), (2,) * 6, 128, page)
+    c.len[0] = 2                       # shorter than the path
+    c.path[1, 2] = 9
+    c.acc[2] = 3                       # beyond the path's room
+    c.len[3] = 129
+    if page:
+        c.table[4, 1] = -1
+    c.lse[5] = float("inf")
+    c.w.fill_(7.0)
+    s = c.score(0.0, "kept")
+    pos = c.pos.clone()
+    c.call(s)
+    bad = [0, 1, 2, 3] + ([4] if page else [])
+    assert c.status.tolist() == [B.S4C_SEQ_BAD_LEN if b in bad else 0 for b in range(6)]
+    for b in bad:
+        assert (c.w[b] == 7.0).all() and torch.equal(c.pos[b], pos[b])
+    assert torch.equal(c.w[5, :, :97], c.win[5, :, :97]) and not c.w[5, :, 97:100].any()
+
+
+def test_weights_far_into_a_large_cache():
+    """More than 2^31 elements of K."""
+    S_cap, n = 1 << 23, 300
+    c = Weigh(5, 3, 6, 4, 1, 128, "bf16", (9, 5, n), (3, 3, 3), 320)
+    small = c.kc
+    c.kc = torch.zeros(3, 1, S_cap, 128, dtype=torch.bfloat16, device="cuda")
+    c.kc[:, :, :320] = small
+    pad = lambda t: torch.cat([t, torch.zeros(3, 1, S_cap - 320, dtype=t.dtype, device="cuda")], 2)
+    win, pos = c.win, c.pos
+    want = None
+    for big in (False, True):
+        if big:
+            c.win, c.pos, c.w = pad(win), pad(pos), torch.full((3, 1, S_cap), 7.0, device="cuda")
+            c.call(c.score(0.0, "kept"), m=S_cap)
+            assert torch.equal(c.w[:, :, :320], want)
+        else:
+            kc, c.kc = c.kc, small
+            c.call(c.score(0.0, "kept"))
+            want, c.kc = c.w.clone(), kc
+
+
+def test_weights_replayed():
+    c = Weigh(6, 3, 30, 8, 4, 128, "f16", (700, 300, 45), (4, 9, 0), 768)
+    s = c.score(9.0, "rows")
+    want = []
+    cases = [((700, 300, 45), (4, 9, 0)), ((10, 768, 1), (9, 1, 0)), ((64, 64, 700), (0, 0, 5))]
+    path = torch.arange(10, **I32).expand(3, 10)
+    c.path.copy_(path)
+    graph = torch.cuda.CUDAGraph()
+    for n, a in cases:
+        c.len.copy_(torch.tensor(n, **I32)); c.acc.copy_(torch.tensor(a, **I32)); c.w.fill_(7.0)
+        c.call(s)
+        want.append(c.w.clone())
+    with torch.cuda.graph(graph):
+        B.s4c_kv_weigh(c.q, c.kc, c.lse, c.len, c.path, c.acc, c.S_cap, s, c.win, c.w, 0.0, c.status)
+    for i in (1, 0, 2, 1):
+        c.len.copy_(torch.tensor(cases[i][0], **I32)); c.acc.copy_(torch.tensor(cases[i][1], **I32)); c.w.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.w, want[i])
+
+
+# ------------------------------------------------------------------------------------------------ eviction
+class Evict:
+    def __init__(self, seed, layers, B_, Hkv, D, dtype, lengths, S_cap, page=0, weights="spread"):
+        r = np.random.default_rng(seed)
+        g = torch.Generator().manual_seed(seed)
+        f = lambda *s: torch.randn(*s, generator=g).to(DT[dtype]).cuda()
+        self.table = None
+        if page:
+            blocks = S_cap // page
+            self.kc, self.vc = f(layers, B_ * blocks + 2, Hkv, page, D), f(layers, B_ * blocks + 2, Hkv, page, D)
+            self.table = torch.from_numpy(r.permutation(B_ * blocks + 2)[:B_ * blocks].reshape(B_, blocks).astype(np.int32)).cuda()
+        else:
+            self.kc, self.vc = f(layers, B_, Hkv, S_cap, D), f(layers, B_, Hkv, S_cap, D)
+        w = {"spread": lambda s: np.exp(2 * r.standard_normal(s)), "ties": lambda s: r.integers(0, 4, s) / 4.0,
+             "equal": lambda s: np.full(s, 0.25), "zero": lambda s: r.choice([0.0, -0.0], s), "signed": lambda s: r.standard_normal(s),
+             "extreme": lambda s: r.choice([0.0, 1e-45, -1e-45, 3e38, np.inf, -np.inf, 1.0, 1.0000001], s)}[weights]((layers, B_, Hkv, S_cap))
+        self.w = torch.from_numpy(w.astype(np.float32)).cuda()
+        pos = np.stack([np.stack([np.stack([r.permutation(2 * S_cap)[:S_cap] for _ in range(Hkv)]) for _ in range(B_)]) for _ in range(layers)])
+        self.pos = torch.from_numpy(pos.astype(np.int32)).cuda()
+        self.next = torch.full((B_,), 2 * S_cap, **I32)
+        self.len = torch.tensor(lengths, **I32)
+        self.layers, self.B, self.Hkv, self.S_cap, self.page = layers, B_, Hkv, S_cap, page
+
+    def rows(self, cache):
+        return torch.stack([torch.from_numpy(K.gather_pages(host(cache[l].view(torch.int16) if cache.dtype != torch.float32 else cache[l]), host(self.table)))
+                            for l in range(self.layers)]) if self.page else cache.cpu()
+
+    def run(self, budget, recent, in_place=False, kept=True, ws=None, sync=True):
+        if in_place:
+            self.w2, self.pos2, self.len2 = self.w, self.pos, self.len
+        else:
+            self.w2, self.pos2, self.len2 = torch.full_like(self.w, 7.0), torch.full_like(self.pos, -7), torch.full_like(self.len, -7)
+        self.kept = torch.full((self.layers, self.B, self.Hkv, budget), -9, **I32) if kept else None
+        self.status = torch.full((self.B,), 9, **I32)
+        ws = B.alloc_workspace(B.s4c_kv_evict_workspace_size(self.layers, self.B, self.Hkv, budget, self.S_cap)) if ws is None else ws
+        args = (self.w, self.pos, self.len, self.next, budget, recent, self.w2, self.pos2, self.len2, ws, self.kept, self.status)
+        if self.page:
+            B.s4c_kv_evict_paged(self.kc, self.vc, self.table, *args)
+        else:
+            B.s4c_kv_evict(self.kc, self.vc, *args)
+        if sync:
+            torch.cuda.synchronize()
+
+    def check(self, budget, recent, in_place=False):
+        before = [self.rows(t).clone() for t in (self.kc, self.vc)]
+        raw = [t.clone() for t in (self.kc, self.vc)]
+        w, pos, n = self.w.clone().cpu(), self.pos.clone().cpu(), self.len.clone()
+        kept, new_len = K.kv_evict(f64(self.w), host(self.pos), host(self.len), host(self.next), budget, recent)
+        self.run(budget, recent, in_place)
+        assert not self.status.any()
+        assert np.array_equal(host(self.kept), kept)
+        assert np.array_equal(host(self.len2), new_len)
+        for cache, old in zip((self.kc, self.vc), before):
+            want = old.clone()
+            for ly, b, g in np.ndindex(self.layers, self.B, self.Hkv):
+                m = int(new_len[b])
+                want[ly, b, g, :m] = old[ly, b, g, torch.from_numpy(kept[ly, b, g, :m]).long()]
+            assert torch.equal(self.rows(cache), want)
+        for got, old, fill in ((self.w2, w, 7.0), (self.pos2, pos, -7)):
+            want = old.clone() if in_place else torch.full_like(old, fill)
+            for ly, b, g in np.ndindex(self.layers, self.B, self.Hkv):
+                m = int(new_len[b])
+                want[ly, b, g, :m] = old[ly, b, g, torch.from_numpy(kept[ly, b, g, :m]).long()]
+            assert torch.equal(got.cpu(), want)
+        if self.page:            # pages that are nobody's
+            used = set(self.table.flatten().tolist())
+            for p in range(self.kc.shape[1]):
+                if p not in used:
+                    assert torch.equal(self.kc[:, p], raw[0][:, p]) and torch.equal(self.vc[:, p], raw[1][:, p])
+
+
+EVICT = {
+    # name: layers, B, Hkv, D, lengths, S_cap, page, budget, recent
+    "lengths around the budget": (1, 5, 2, 64, (0, 1, 30, 31, 32), 40, 0, 31, 7),
+    "one row stays": (1, 2, 3, 128, (64, 5), 64, 0, 1, 0),
+    "one row goes": (2, 2, 2, 64, (65, 64), 65, 0, 64, 64),
+    "layers": (3, 2, 2, 128, (700, 333), 768, 0, 300, 50),
+    "over a wave's rows, odd": (1, 1, 2, 64, (4099,), 4101, 0, 2051, 513),
+    "most rows go": (1, 2, 1, 128, (3000, 2999), 3000, 0, 17, 3),
+    "paged": (2, 3, 2, 64, (200, 64, 511), 512, 64, 129, 20),
+    "budget beyond the cache": (1, 2, 2, 64, (40, 20), 40, 0, 100, 100),
+}
+
+
+@pytest.mark.parametrize("weights", ["spread", "ties", "equal", "zero", "signed", "extreme"])
+@pytest.mark.parametrize("name", EVICT)
+def test_eviction_against_the_definition(name, weights):
+    layers, B_, Hkv, D, lengths, S_cap, page, budget, recent = EVICT[name]
+    if weights not in ("spread", "ties") and S_cap > 1000:
+        lengths, S_cap, budget, recent = tuple(min(n, 900) for n in lengths), 900, min(budget, 450), min(recent, 100)
+    for dtype, in_place in (("bf16", False), ("f32", True)):
+        c = Evict(sum(map(ord, name + weights)), layers, B_, Hkv, D, dtype, lengths, S_cap, page, weights)
+        c.check(budget, recent, in_place)
+
+
+def test_eviction_of_long_units():
+    """Lengths on both sides of what a workgroup keeps in registers."""
+    for n, budget in ((32768, 20000), (32769, 32000), (70001, 30011)):
+        c = Evict(n, 1, 2, 1, 64, "bf16", (n, n - 9000), n, 0, "ties")
+        c.check(budget, 999)
+
+
+def test_evicted_twice():
+    """The second time the rows lie in no order: recent ones are found by their positions."""
+    c = Evict(2, 2, 2, 2, 64, "f16", (500, 450), 512)
+    c.check(400, 100, in_place=True)
+    c.check(200, 60, in_place=True)
+    assert c.len.tolist() == [200, 200]
+    new = c.pos >= c.next.view(1, -1, 1, 1) - 60
+    assert new[..., :200].sum() > 0
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_eviction_of_flagged_sequences(page):
+    c = Evict(3, 2, 4, 2, 64, "bf16", (100, 128, 90, 80), 128, page)
+    c.len[1], c.len[2] = 129, -3
+    if page:
+        c.table[3, 0] = c.kc.shape[1]
+    raw = [t.clone() for t in (c.kc, c.vc)]
+    c.run(50, 10)
+    bad = [1, 2] + ([3] if page else [])
+    assert c.status.tolist() == [B.S4C_SEQ_BAD_LEN if b in bad else 0 for b in range(4)]
+    assert c.len2.tolist() == [50, 129, -3, 80 if page else 50]
+    for b in bad:
+        assert (c.w2[:, b] == 7.0).all() and (c.pos2[:, b] == -7).all() and (c.kept[:, b] == -1).all()
+        if not page:
+            assert torch.equal(c.kc[:, b], raw[0][:, b]) and torch.equal(c.vc[:, b], raw[1][:, b])
+
+
+def test_eviction_without_kept_and_status_replayed():
+    c = Evict(4, 1, 3, 4, 128, "bf16", (600, 513, 300), 640)
+    ws = B.alloc_workspace(B.s4c_kv_evict_workspace_size(1, 3, 4, 256, 640))
+    w2, pos2, n2 = torch.zeros_like(c.w), torch.zeros_like(c.pos), torch.zeros_like(c.len)
+    kc, vc = c.kc.clone(), c.vc.clone()
+    call = lambda: B.s4c_kv_evict(c.kc, c.vc, c.w, c.pos, c.len, c.next, 256, 40, w2, pos2, n2, ws)
+    lengths = [(600, 513, 300), (10, 640, 257), (640, 640, 640)]
+    want = []
+    for n in lengths:
+        c.kc.copy_(kc); c.vc.copy_(vc); c.len.copy_(torch.tensor(n, **I32)); w2.zero_(); pos2.zero_()
+        call()
+        want.append([t.clone() for t in (c.kc, c.vc, w2, pos2, n2)])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in (2, 0, 1, 2):
+        c.kc.copy_(kc); c.vc.copy_(vc); c.len.copy_(torch.tensor(lengths[i], **I32)); w2.zero_(); pos2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((c.kc, c.vc, w2, pos2, n2), want[i]):
+            assert torch.equal(got, w)
+
+
+def test_eviction_from_a_large_cache():
+    """More than 2^31 elements: the second sequence's rows."""
+    S_cap = 9 << 20
+    k = torch.zeros(1, 2, 1, S_cap, 128, dtype=torch.float16, device="cuda")
+    c = Evict(5, 1, 2, 1, 128, "f16", (700, 650), 704)
+    k[..., :704, :] = c.kc
+    v = torch.zeros_like(k)
+    v[..., :704, :] = c.vc
+    pad = lambda t: torch.cat([t, torch.zeros(1, 2, 1, S_cap - 704, dtype=t.dtype, device="cuda")], 3)
+    w, pos, n = pad(c.w), pad(c.pos), c.len.clone()
+    ws = B.alloc_workspace(B.s4c_kv_evict_workspace_size(1, 2, 1, 333, S_cap))
+    B.s4c_kv_evict(k, v, w, pos, n, c.next, 333, 50, w, pos, n, ws)
+    c.check(333, 50, in_place=True)
+    assert torch.equal(k[..., :704, :], c.kc) and torch.equal(v[..., :704, :], c.vc)
+    assert torch.equal(w[..., :333], c.w[..., :333]) and torch.equal(pos[..., :333], c.pos[..., :333]) and torch.equal(n, c.len)
+
+
+def test_refusals():
+    c = Weigh(7, 2, 6, 4, 2, 64, "bf16", (50, 20), (1, 2), 64)
+    call = lambda score=B.PLAIN_SCORE, lse=c.lse, path=c.path, w=c.w, m=64, length=c.len, q=c.q: B.s4c_kv_weigh(
+        q, c.kc, lse, length, path, c.acc, m, score, c.win, w, 0.0, c.status)
+    call()
+    for kw in (dict(lse=c.lse.double()), dict(lse=c.lse[:, :5].contiguous()), dict(path=c.path.long()), dict(w=c.w[:, :, :63].contiguous()),
+               dict(length=c.len[:1]), dict(q=c.q.half()), dict(score=B.Score(0.0, None, c.pos[:, :1].contiguous(), c.root))):
+        with pytest.raises(TypeError):
+            call(**kw)
+    for m in (0, 65):
+        with pytest.raises(B.S4CError) as e:
+            call(m=m)
+        assert e.value.code == -2
+    with pytest.raises(B.S4CError) as e:
+        call(score=B.Score(-2.0))
+    assert e.value.code == -2
+    with pytest.raises(B.S4CError) as e:
+        call(score=B.Score(0.0, None, c.pos))
+    assert e.value.code == -1
+    with pytest.raises(ValueError):
+        call(lse=c.lse.cpu())
+    d = Evict(6, 1, 2, 2, 64, "bf16", (60, 50), 64)
+    ws = B.alloc_workspace(B.s4c_kv_evict_workspace_size(1, 2, 2, 32, 64))
+    ev = lambda budget=32, recent=4, ws=ws, w=d.w, pos=d.pos, n=d.len, kept=None: B.s4c_kv_evict(d.kc, d.vc, w, pos, n, d.next, budget, recent, w,
+                                                                                              pos, d.len, ws, kept)
+    for kw in (dict(budget=0, recent=0), dict(recent=33), dict(recent=-1)):
+        with pytest.raises(B.S4CError) as e:
+            ev(**kw)
+        assert e.value.code == -2
+    for bad in (None, ws[:-1]):
+        with pytest.raises(B.S4CError) as e:
+            ev(ws=bad)
+        assert e.value.code == -4
+    for kw in (dict(w=d.w.half()), dict(pos=d.pos.long()), dict(n=d.len.long()), dict(kept=torch.zeros(1, 2, 2, 31, **I32))):
+        with pytest.raises(TypeError):
+            ev(**kw)
+    ev()
+    assert d.len.tolist() == [32, 32]
+
+
+# ------------------------------------------------------------------------------------------------ all together
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_conversation_over_a_bounded_cache(dtype):
+    """Ten steps of two layers: attention with changed scores, acceptance, commit, weights, and eviction whenever a sequence may grow
+    over the cache.  Every step's results against the definitions on what the GPU holds before it."""
+    Ly, Bn, N, Hq, Hkv, D, V, depth = 2, 2, 9, 4, 2, 64, 50, 4
+    budget, recent, S_cap = 40, 12, 56
+    dt = DT[dtype]
+    g = torch.Generator().manual_seed(3)
+    f = lambda *s: torch.randn(*s, generator=g).to(dt).cuda()
+    v = TreeVerifier(Bn, N, Hq, Hkv, D, S_cap, V, dt, depth, S_cap, layers=Ly, budget=budget, recent=recent)
+    kc, vc = f(Ly, Bn, Hkv, S_cap, D), f(Ly, Bn, Hkv, S_cap, D)
+    n = torch.tensor([30, 44], **I32)
+    weight = torch.rand(Ly, Bn, Hkv, S_cap, generator=g).cuda()
+    pos = torch.arange(S_cap, **I32).repeat(Ly, Bn, Hkv, 1)
+    root = n.clone()
+    slopes = torch.tensor([0.5, 0.25, 0.125, 0.0625], device="cuda")
+    parent = torch.tensor([[-1, 0, 0, 1, 1, 2, 3, 4, 6][:N]] * Bn, **I32).clamp(max=N)
+    parent[:, 8] = 5
+    evicted = 0
+    for step in range(10):
+        logits = f(Bn, N, V)
+        tokens = torch.randint(0, V, (Bn, N), generator=g).to(torch.int32).cuda()
+        for b in range(Bn):                      # some path is accepted
+            up = int(torch.randint(0, 3, (1,), generator=g))
+            for node in [3, 6, 1][:up] + ([1] if up else []):
+                tokens[b, node] = logits[b, int(parent[b, node])].argmax().to(torch.int32)
+        kt, vt = f(Ly, Bn, N, Hkv, D), f(Ly, Bn, N, Hkv, D)
+        qs, lses = [], []
+        for ly in range(Ly):
+            q, out, lse = f(Bn, N, Hq, D), torch.empty(Bn, N, Hq, D, dtype=dt, device="cuda"), torch.empty(Bn, N, Hq, device="cuda")
+            score = B.Score(6.0, slopes, pos[ly], root)
+            v.tree_attn_scored(q, kt[ly], vt[ly], kc[ly], vc[ly], n, parent, score, out=out, lse=lse)
+            want = K.tree_attn_scored(f64(q), f64(kt[ly]), f64(vt[ly]), f64(kc[ly]), f64(vc[ly]), host(n), host(parent), 0.0, 6.0,
+                                      f64(slopes), host(pos[ly]), host(root))
+            # scores: 64 additions of sum |q k| / 8 < 16, 2^-24 each: 6e-5; two roundings of half a step beside it
+            assert np.abs(f64(out) - want[0]).max() <= (torch.finfo(dt).eps + 1e-4) * (1 + np.abs(want[0]).max())
+            assert np.abs(f64(lse) - want[1]).max() <= 1e-4
+            qs.append(q)
+            lses.append(lse)
+        v.accept_path(logits, parent, tokens, B.S4C_GREEDY)
+        v.commit_path(kt, vt, kc, vc, n)
+        for ly in range(Ly):
+            score = B.Score(6.0, slopes, pos[ly], root)
+            w, p, _ = K.kv_weigh(f64(qs[ly]), f64(kc[ly]), f64(lses[ly]), host(n), host(v.path), host(v.accept_len), f64(weight[ly]), 0.0, 6.0,
+                                 f64(slopes), host(pos[ly]), host(root))
+            v.kv_weigh(qs[ly], kc[ly], n, score, weight[ly], lse=lses[ly])
+            for b in range(Bn):
+                assert np.allclose(f64(weight[ly])[b, :, :int(n[b])], w[b, :, :int(n[b])], rtol=1e-4, atol=1e-5)
+            assert np.array_equal(host(pos[ly]), p)
+        root += v.accept_len + 1
+        assert not (v.attn_status.any() or v.accept_status.any() or v.compact_status.any() or v.weigh_status.any())
+        if int(n.max()) + depth > S_cap:
+            kept, new_len = K.kv_evict(f64(weight), host(pos), host(n), host(root), budget, recent)
+            old = kc.clone()
+            v.kv_evict(kc, vc, weight, pos, n, root)
+            assert np.array_equal(host(v.kept), kept) and np.array_equal(host(n), new_len)
+            for ly, b, h in np.ndindex(Ly, Bn, Hkv):
+                m = int(n[b])
+                assert torch.equal(kc[ly, b, h, :m], old[ly, b, h, torch.from_numpy(kept[ly, b, h, :m]).long().cuda()])
+                assert len(set(pos[ly, b, h, :m].tolist())) == m and int(pos[ly, b, h, :m].max()) == int(root[b]) - 1
+            evicted += 1
+    assert evicted >= 2
+
+
+def test_step_with_a_score_is_the_three_calls():
+    Bn, N, Hq, Hkv, D, S_cap, V = 2, 10, 4, 2, 128, 300, 64
+    g = torch.Generator().manual_seed(9)
+    f = lambda *s: torch.randn(*s, generator=g).to(torch.bfloat16).cuda()
+    q, kt, vt, kc, vc, logits = f(Bn, N, Hq, D), f(Bn, N, Hkv, D), f(Bn, N, Hkv, D), f(Bn, Hkv, S_cap, D), f(Bn, Hkv, S_cap, D), f(Bn, N, V)
+    parent = torch.tensor([[-1] + [max(0, i - 2) for i in range(1, N)]] * Bn, **I32)
+    tokens = torch.randint(0, V, (Bn, N), generator=g).to(torch.int32).cuda()
+    tokens[:, 1] = logits[:, 0].float().argmax(-1).to(torch.int32)
+    s = B.Score(20.0, torch.rand(Hq, generator=g).cuda())
+    got = []
+    for whole in (True, False):
+        v = TreeVerifier(Bn, N, Hq, Hkv, D, S_cap, V, torch.bfloat16, N, 256)
+        k, w, n = kc.clone(), vc.clone(), torch.tensor([250, 100], **I32)
+        if whole:
+            v.step(q, kt, vt, k, w, n, parent, logits, tokens, B.S4C_GREEDY, score=s)
+        else:
+            v.tree_attn_scored(q, kt, vt, k, w, n, parent, s)
+            v.accept_path(logits, parent, tokens, B.S4C_GREEDY)
+            v.kv_compact(kt, vt, k, w, n)
+        got.append((v.out, v.lse, v.path, v.accept_len, k, w, n))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert got[0][3].min() >= 1

@@ -3,11 +3,16 @@
 //   x = scale q.k;   cap > 0: x <- cap tanh(x / cap);   slopes: x <- x + slope[head] (position of the key - position of the root)
 //
 // In log2 units throughout.  The distance is counted from the root and not from the row's node: the difference is the same for all
-// keys of a row, and the softmax does not see it.  The cap is where the work is: a tile's scores are C y p(y^2) with y = x / cap, C =
-// cap log2(e) and p the fifth-order fit of tanh(y)/y on |y| <= 0.6 (relative error 7.5e-8, least at Chebyshev nodes), seven operations a
-// score without a transcendental one, which run at a quarter of the rate.  Where some score of the wave lies beyond, those are
-// C - 2 C / (1 + exp2(2 log2(e) y)), off by C 2^-23, a relative 2.2e-7 there.
-// Positions are differences of 32-bit integers first and fp32 after: exact up to 2^24.
+// keys of a row, and the softmax does not see it.  Positions are differences of 32-bit integers first and fp32 after: exact up to 2^24.
+//
+// What it costs is operations of the vector ALUs, of which a score otherwise has about eight (four of them its exponential):
+//   bias by rows      one: the tile's own distance goes to the reference that the exponentials are taken against, a key's distance inside the
+//                     tile is a constant; the bias is added to the bare product (slopes are divided by the scale once)
+//   bias looked up    three: difference, conversion, addition
+//   cap               C y p(y^2), y = x / cap, C = cap log2(e), p a fit of tanh(y)/y at Chebyshev nodes.  Where all scores of a wave are within 0.35
+//                     of the cap (and nothing is added), the kernel for many rows takes four terms (relative error 3.5e-8) with the scale in the
+//                     coefficients, and the last product is the one that makes the exponent: four more operations.  Within 0.6 five terms (7.5e-8).  Beyond, C - 2 C / (1 +
+//                     exp2(2 log2(e) y)), two more operations at a quarter of the rate, off by C 2^-23, a relative 2.2e-7 there.
 #pragma once
 #include "common.h"
 
@@ -37,71 +42,96 @@ __device__ __forceinline__ float beyond(float y, float c) {
     return fmaf(-2.f * c, __builtin_amdgcn_rcpf(1.f + e), c);
 }
 
-// products -> capped scores in log2 units; N values, V(j) a reference to the j-th
+// products -> capped scores in log2 units (cap > 0); N values, s(j) a reference to the j-th
 template <int N, class V>
-__device__ __forceinline__ void change_all(V s, const Args<kChanged>& a, float scale_log2) {
-    if (a.cap_log2 > 0.f) {
-        float most = 0.f;
+__device__ __forceinline__ void cap_all(V s, const Changed& a) {
+    float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            s(j) *= a.to_y;
-            most = fmaxf(most, fabsf(s(j)));
-        }
-        if (!__any(most > kFitUpTo)) {
+    for (int j = 0; j < N; ++j) {
+        s(j) *= a.to_y;
+        most = fmaxf(most, fabsf(s(j)));
+    }
+    if (!__any(most > kFitUpTo)) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) s(j) = fitted(s(j), a.cap_log2);
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) s(j) = fabsf(s(j)) <= kFitUpTo ? fitted(s(j), a.cap_log2) : beyond(s(j), a.cap_log2);
-        }
+        for (int j = 0; j < N; ++j) s(j) = fitted(s(j), a.cap_log2);
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) s(j) *= scale_log2;
+        for (int j = 0; j < N; ++j) s(j) = fabsf(s(j)) <= kFitUpTo ? fitted(s(j), a.cap_log2) : beyond(s(j), a.cap_log2);
     }
 }
 // ... of a tile of 32 keys (a lane's register j), and of NG blocks of 16 x 16
-__device__ __forceinline__ void change(f32x16& s, const Args<kChanged>& a, float scale_log2) {
+__device__ __forceinline__ void cap(f32x16& s, const Changed& a) {
     float x[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = s[j];
-    change_all<16>([&](int j) -> float& { return x[j]; }, a, scale_log2);
+    cap_all<16>([&](int j) -> float& { return x[j]; }, a);
 #pragma unroll
     for (int j = 0; j < 16; ++j) s[j] = x[j];
 }
 template <int NG>
-__device__ __forceinline__ void change(f32x4 (&s)[NG], const Args<kChanged>& a, float scale_log2) {
+__device__ __forceinline__ void cap(f32x4 (&s)[NG], const Changed& a) {
     float x[4 * NG];
 #pragma unroll
     for (int j = 0; j < 4 * NG; ++j) x[j] = s[j >> 2][j & 3];
-    change_all<4 * NG>([&](int j) -> float& { return x[j]; }, a, scale_log2);
+    cap_all<4 * NG>([&](int j) -> float& { return x[j]; }, a);
 #pragma unroll
     for (int j = 0; j < 4 * NG; ++j) s[j >> 2][j & 3] = x[j];
 }
+// What a value of a tile is multiplied with to be a score in log2 units.  FIT: a product within fit_up_to is capped by it, s p(s^2) in
+// all; one that has been capped otherwise is multiplied by 1 with the same instructions, so that one line of code lies behind the choice.
+template <bool FIT>
+struct Factor {
+    float c[4];
+    __device__ __forceinline__ Factor(const Changed& a, bool fits, float)
+        : c{fits ? a.fit[0] : 1.f, fits ? a.fit[1] : 0.f, fits ? a.fit[2] : 0.f, fits ? a.fit[3] : 0.f} {}
+    __device__ __forceinline__ float operator()(float s) const {
+        const float z = s * s;
+        return fmaf(z, fmaf(z, fmaf(z, c[3], c[2]), c[1]), c[0]);
+    }
+};
+template <>
+struct Factor<false> {
+    float mul;
+    template <class Score>
+    __device__ __forceinline__ Factor(const Score&, bool, float m) : mul(m) {}
+    __device__ __forceinline__ float operator()(float) const { return mul; }
+};
 
-// Register j of a lane is key 8 (j/4) + j%4 of the lane's part of a tile.
-// ... whose first key is row `first` before (< 0) or behind the root
-__device__ __forceinline__ void add_rows(f32x16& s, float slope, int first) {
-    const float f = (float)first;
+// Register j of a lane is key 8 (j/4) + j%4 of the lane's part of a block of 32; a tile has BLOCKS of them.
+// ... whose first key is row `first` before (< 0) or behind the root; returns what is left to add to the lane's scores, in log2 units.
+// (Counted from the part's last key, the one next to the root: there the sums are small, and so are their roundings.)
+template <int BLOCKS>
+__device__ __forceinline__ float add_rows(f32x16 (&s)[BLOCKS], float slope, int first, const Changed& a) {
+    constexpr int kLast = 32 * BLOCKS - 5;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s[j] = fmaf(slope, f + (float)(8 * (j >> 2) + (j & 3)), s[j]);
+    for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[k][j] = fmaf((float)(32 * k + 8 * (j >> 2) + (j & 3) - kLast), slope, s[k][j]);
+    return slope * a.mul * (float)(first + kLast);
 }
 // ... whose positions lie in LDS
-__device__ __forceinline__ void add_looked_up(f32x16& s, float slope, const int32_t* pos, int root) {
+template <int BLOCKS>
+__device__ __forceinline__ void add_looked_up(f32x16 (&s)[BLOCKS], float slope, const int32_t* pos, int root) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const i32x4 p = *(const i32x4*)(pos + 8 * q);
+    for (int k = 0; k < BLOCKS; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, (float)(p[e] - root), s[4 * q + e]);
-    }
+        for (int q = 0; q < 4; ++q) {
+            const i32x4 p = *(const i32x4*)(pos + 32 * k + 8 * q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[k][4 * q + e] = fmaf(slope, (float)(p[e] - root), s[k][4 * q + e]);
+        }
 }
 // ... of nodes of the tree
-__device__ __forceinline__ void add_depths(f32x16& s, float slope, const float* depth) {
+template <int BLOCKS>
+__device__ __forceinline__ void add_depths(f32x16 (&s)[BLOCKS], float slope, const float* depth) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const f32x4 d = *(const f32x4*)(depth + 8 * q);
+    for (int k = 0; k < BLOCKS; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, d[e], s[4 * q + e]);
-    }
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 d = *(const f32x4*)(depth + 32 * k + 8 * q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[k][4 * q + e] = fmaf(slope, d[e], s[k][4 * q + e]);
+        }
 }
 // every node's depth, by the thread that has written its ancestors
 __device__ __forceinline__ void note_depth(const AttnArgs& a, const uint32_t* anc, float* depth) {
@@ -121,8 +151,8 @@ struct Writer {
         if (lse) lse[row] = l > 0.f ? (m - shift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : INFINITY;
     }
 };
-__device__ __forceinline__ work::NoRowDone writer(const Args<kPlain>&, float) { return {}; }
-__device__ __forceinline__ Writer writer(const Args<kChanged>& a, float shift) { return {a.lse, shift}; }
+__device__ __forceinline__ work::NoRowDone writer(const Unchanged&, float) { return {}; }
+__device__ __forceinline__ Writer writer(const Changed& a, float shift) { return {a.lse, shift}; }
 
 }  // namespace score
 }  // namespace s4c

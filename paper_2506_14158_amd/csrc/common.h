@@ -96,17 +96,20 @@ hipError_t launch_smallm_f16(const AttnArgs& a, const StepTail<kGreedyStep>* ste
 hipError_t launch_smallm_f32(const AttnArgs& a, const StepTail<kGreedyStep>* step, hipStream_t st);
 hipError_t launch_attn_merge(const AttnArgs& a, int dtype, hipStream_t st);
 // the same with changed scores (attn_score.h)
-namespace score {
-enum Kind { kPlain = 0, kChanged = 1 };
-template <Kind KIND>
-struct Args;
-}
-hipError_t launch_tree_attn_large_scored(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
-hipError_t launch_tree_attn_small_scored(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
-hipError_t launch_large_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
-hipError_t launch_smallm_scored_bf16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
-hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st);
-hipError_t launch_attn_merge(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st);
+namespace score { struct Changed; }
+hipError_t launch_tree_attn_large_scored(const AttnArgs& a, int dtype, const score::Changed& sc, hipStream_t st);
+hipError_t launch_tree_attn_small_scored(const AttnArgs& a, int dtype, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_lse_bf16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_lse_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_slopes_bf16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_slopes_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_cap_bf16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_cap_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_cap_slopes_bf16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_large_cap_slopes_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_smallm_scored_bf16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st);
+hipError_t launch_attn_merge(const AttnArgs& a, int dtype, const score::Changed& sc, hipStream_t st);
 AttnTile attn_tile_large(const s4c_attn_shape& s);
 AttnTile attn_tile_small(const s4c_attn_shape& s, int32_t max_cache_len, int cus);
 
@@ -193,19 +196,25 @@ struct CompactArgs {
 };
 hipError_t launch_compact(const CompactArgs& a, hipStream_t st);
 
-// How attention scores are changed (attn_score.h), as kernels take it.
+// How attention scores are changed (attn_score.h), as kernels take it.  The kernel for few rows has one kind for all changes; the
+// one for many, where operations count, one for none (but the log-sum-exp), for slopes, for a cap and for both.
 namespace score {
-template <>
-struct Args<kPlain> {};
-template <>
-struct Args<kChanged> {
+enum Kind { kPlain, kAny, kLse, kSlopes, kCap, kCapSlopes };
+struct Changed {
     const float* slopes;         // [Hq] or null
     const int32_t* key_pos;      // [B][Hkv][S_cap] or null: row j has position j, the root cache_len
     const int32_t* root_pos;     // [B], with key_pos
     float* lse;                  // [B][N][Hq] or null
     float cap_log2;              // cap log2(e); 0: none
     float to_y;                  // scale / cap
+    float mul;                   // from what a tile's values are after the cap to log2 units: 1, or scale log2(e) where there is no cap
+    float slope_mul;             // log2(e) / mul
+    float fit[4], fit_up_to;     // cap log2(e) tanh(to_y s) = s (fit[0] + s^2 (fit[1] + ..)) for |s| <= fit_up_to (0: not used)
 };
+struct Unchanged {};
+template <Kind KIND> struct ArgsOf { typedef Changed type; };
+template <> struct ArgsOf<kPlain> { typedef Unchanged type; };
+template <Kind KIND> using Args = typename ArgsOf<KIND>::type;
 }  // namespace score
 
 struct WeighArgs {
@@ -219,8 +228,7 @@ struct WeighArgs {
     float* weight;
     int32_t* key_pos;            // score.key_pos, to write the path's
     int32_t* status;
-    score::Args<score::kChanged> score;
-    float scale_log2;
+    score::Changed score;
     int32_t B, Hq, Hkv, D, N, S_cap, G, max_path, max_cache_len, cus;
     const int32_t* block_table;  // as in AttnArgs
     int32_t max_blocks, page_shift, num_pages;
@@ -242,6 +250,7 @@ struct EvictArgs {
     int2* meta;                  // [units] rows that move, rows that stay
     int32_t* lists;              // [units][2][list_len] places, and the rows that move there
     int32_t layers, B, Hkv, S_cap, budget, recent, list_len, row_bytes, cus;
+    int32_t lds_keys;            // set by the launcher: rows whose keys fit in LDS
     const int32_t* block_table;
     int32_t max_blocks, page_shift, num_pages;
 };

@@ -5,171 +5,69 @@
 // lies behind the budget and every place before it, so rows move in any order, in place, and no more of them than must.  (Attention does
 // not ask for an order of the keys; what depends on a row's age reads its position.)
 //
-// Two launches.  evict_select_kernel, a workgroup per unit, finds the smallest key that stays by a radix descent (histograms of 11, 11 and
-// 10 bits; a key is the total's bits in integer order, all ones for recent rows) and lists places and movers in row order.
-// evict_move_kernel copies the rows: bound by the memory.
-#include "common.h"
+// Selection, a workgroup per unit.  A row's key is its total's bits in integer order, all ones if it is recent; the keys of up to 32768 rows
+// are kept in LDS (longer units are read again for every sweep).  The smallest key that stays is found by a radix descent, 11, 11
+// and 10 bits from the top: a histogram in LDS, which every wave scans by itself (a barrier less, and nothing to hand over), and the last digits are
+// left out where all rows of a bin stay, as they do as soon as totals differ.  Places and movers are listed in row order by ballots.  What bounds it is
+// the instructions of one CU on a long unit (32768 rows: 52 us before keys were looked at as few times and with as few instructions as they are now).
+// Moving is a copy, bound by memory.
+#include "mfma_common.h"
 
 namespace s4c {
 
 namespace {
 
-constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
-constexpr int kBins = 2048, kCopies = 4;
-constexpr int kMove = 256;
+constexpr int kBins = 2048;
+constexpr int kMostKeys = 32768;             // in LDS
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
-    return x;
-}
-
-// a total's bits in the order of the numbers, below all ones; -0 as 0
+// a total's bits in the order of the numbers, 1 .. 2^32 - 2 (-0 as 0); recent rows: 2^32 - 1; 0 is no row's
 __device__ __forceinline__ uint32_t key_of(float w, bool recent) {
     const uint32_t u = __float_as_uint(w + 0.f);
     const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-    return recent ? 0xFFFFFFFFu : k < 0xFFFFFFFEu ? k : 0xFFFFFFFEu;
+    return recent ? 0xFFFFFFFFu : min(max(k, 1u), 0xFFFFFFFEu);
 }
 
-__global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[kCopies][kBins];
-    __shared__ uint32_t s_wave[4][kSelectWaves];
-    __shared__ uint32_t s_pick[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int unit = blockIdx.x, b = (unit / a.Hkv) % a.B;
-    const int n = a.cache_len[b];
-    bool bad = n < 0 || n > a.S_cap;
-    if (!bad && a.block_table)
-        for (int i = tid; i < (n + (1 << a.page_shift) - 1) >> a.page_shift; i += kSelect) {
-            const int id = a.block_table[(size_t)b * a.max_blocks + i];
-            bad = bad || id < 0 || id >= a.num_pages;
-        }
-    bad = __syncthreads_or(bad) != 0;
-    const int m = min(n, a.budget);
-    const size_t row0 = (size_t)unit * a.S_cap;
-    const float* w = a.weight + row0;
-    const int32_t* pos = a.key_pos + row0;
-    int32_t* kept = a.kept ? a.kept + (size_t)unit * a.budget : nullptr;
-    if (a.status && unit < a.B * a.Hkv && unit % a.Hkv == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
-    const bool apart = a.weight_out != a.weight, pos_apart = a.key_pos_out != a.key_pos;
-    if (bad || n <= a.budget) {
-        if (tid == 0) a.meta[unit] = make_int2(0, n);
-        if (kept)
-            for (int j = tid; j < a.budget; j += kSelect) kept[j] = !bad && j < n ? j : -1;
-        if (!bad)
-            for (int j = tid; j < n; j += kSelect) {
-                if (apart) a.weight_out[row0 + j] = w[j];
-                if (pos_apart) a.key_pos_out[row0 + j] = pos[j];
-            }
-        return;
-    }
-    const int newest = a.next_pos[b] - a.recent;
-    auto key_at = [&](int j) { return key_of(w[j], pos[j] >= newest); };
+// Where bin d of a histogram lies: a scanning lane l reads bins 32 l .. 32 l + 31, each time all lanes from different banks.
+__device__ __forceinline__ uint32_t bin_at(uint32_t d) { return d ^ (d >> 5); }
 
-    // ---- the m-th largest key, from its highest bits down; `left`: how many of the keys with these bits stay
-    uint32_t prefix = 0, left = (uint32_t)m;
-    int shift = 32;
-#pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-        const int bits = pass < 2 ? 11 : 10, lower = shift - bits;
-        for (int i = tid; i < kCopies * kBins; i += kSelect) ((uint32_t*)hist)[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += kSelect) {
-            const uint32_t k = key_at(j);
-            if (pass == 0 || (k >> shift) == prefix) atomicAdd(&hist[lane & (kCopies - 1)][(k >> lower) & ((1u << bits) - 1u)], 1u);
+// One more in bin d for every lane that is `on`.  Lanes that add to one word wait for each other; CROWDED, where most keys may share a bin, one lane
+// adds for all if all agree.
+template <bool CROWDED>
+__device__ __forceinline__ void count(uint32_t* hist, bool on, uint32_t d) {
+    if constexpr (CROWDED) {
+        const unsigned long long who = __ballot(on);
+        if (who == 0) return;
+        const int one = __ffsll((long long)who) - 1;
+        if (__ballot(on && d == __builtin_amdgcn_readlane(d, one)) == who) {
+            if ((int)(threadIdx.x & 63) == one) atomicAdd(&hist[bin_at(d)], (uint32_t)__popcll(who));
+            return;
         }
-        __syncthreads();
-        // thread i has the i-th pair of bins from the top
-        const int top = kBins - 1 - 2 * tid;
-        uint32_t h0 = 0, h1 = 0;
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) { h0 += hist[c][top]; h1 += hist[c][top - 1]; }
-        uint32_t incl = h0 + h1;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t y = __shfl_up(incl, off);
-            if (lane >= off) incl += y;
-        }
-        if (lane == 63) s_wave[0][wave] = incl;
-        __syncthreads();
-        uint32_t before = 0;
-        for (int i = 0; i < wave; ++i) before += s_wave[0][i];
-        const uint32_t above = before + incl - h0 - h1;              // keys in higher bins
-        if (above < left && left <= above + h0) { s_pick[0] = top; s_pick[1] = left - above; }
-        else if (above + h0 < left && left <= above + h0 + h1) { s_pick[0] = top - 1; s_pick[1] = left - above - h0; }
-        __syncthreads();
-        prefix = (prefix << bits) | s_pick[0];
-        left = s_pick[1];
-        shift = lower;
-        __syncthreads();
     }
-    const uint32_t least = prefix;                                     // rows of larger keys stay, and the first `left` of this one
+    if (on) atomicAdd(&hist[bin_at(d)], 1u);
+}
 
-    // ---- a wave has a run of rows: how many of them stay before and behind the budget
-    const int run = (n + kSelectWaves * 64 - 1) / (kSelectWaves * 64) * 64, j0 = wave * run, j1 = min(n, j0 + run);
-    uint32_t more_front = 0, same_front = 0, more_back = 0, same_back = 0;
-    for (int j = j0 + lane; j < j1; j += 64) {
-        const uint32_t k = key_at(j);
-        if (j < m) { more_front += k > least; same_front += k == least; }
-        else { more_back += k > least; same_back += k == least; }
-    }
-    more_front = wave_sum(more_front); same_front = wave_sum(same_front);
-    more_back = wave_sum(more_back); same_back = wave_sum(same_back);
-    if (lane == 0) { s_wave[0][wave] = more_front; s_wave[1][wave] = same_front; s_wave[2][wave] = more_back; s_wave[3][wave] = same_back; }
-    __syncthreads();
-    uint32_t same = 0, hole = 0, mover = 0, movers = 0;                // before this wave's rows; of the unit
-    {
-        uint32_t seen = 0, movers_so_far = 0;
-        for (int i = 0; i < kSelectWaves; ++i) {
-            if (i == wave) { same = seen; mover = movers_so_far; }
-            const uint32_t front = s_wave[1][i], back = s_wave[3][i];
-            const uint32_t keep_front = s_wave[0][i] + min(front, left - min(left, seen));
-            seen += front;
-            const uint32_t keep_back = s_wave[2][i] + min(back, left - min(left, seen));
-            seen += back;
-            const int f0 = min(m, i * run), f1 = min(m, (i + 1) * run);
-            if (i < wave) hole += (uint32_t)(f1 - f0) - keep_front;
-            movers_so_far += keep_back;
-        }
-        movers = movers_so_far;
-    }
-    if (tid == 0) a.meta[unit] = make_int2((int)movers, m);
-
-    // ---- the lists, in row order
-    int32_t* holes = a.lists + (size_t)unit * 2 * a.list_len;
-    int32_t* from = holes + a.list_len;
-    const unsigned long long below = (1ull << lane) - 1;
-    for (int j = j0 + lane; __any(j < j1); j += 64) {
-        const bool on = j < j1;
-        const uint32_t k = on ? key_at(j) : 0u;
-        const unsigned long long eq = __ballot(on && k == least);
-        const bool stays = on && (k > least || (k == least && same + __popcll(eq & below) < left));
-        same += __popcll(eq);
-        const bool is_hole = on && !stays && j < m, moves = stays && j >= m;
-        const unsigned long long bh = __ballot(is_hole), bm = __ballot(moves);
-        if (is_hole) holes[hole + __popcll(bh & below)] = j;
-        if (moves) from[mover + __popcll(bm & below)] = j;
-        hole += __popcll(bh);
-        mover += __popcll(bm);
-        if (stays && j < m) {
-            if (kept) kept[j] = j;
-            if (apart) a.weight_out[row0 + j] = w[j];
-            if (pos_apart) a.key_pos_out[row0 + j] = pos[j];
-        }
+// n words from `from` to `to`, by the threads of a workgroup
+template <int THREADS>
+__device__ __forceinline__ void copy_words(uint32_t* to, const uint32_t* from, int n) {
+    if (((((uintptr_t)to) | ((uintptr_t)from)) & 15) == 0) {
+        for (int i = threadIdx.x; i < n / 4; i += THREADS) ((u32x4*)to)[i] = ((const u32x4*)from)[i];
+        const int i = n / 4 * 4 + threadIdx.x;
+        if (i < n) to[i] = from[i];
+    } else {
+        for (int i = threadIdx.x; i < n; i += THREADS) to[i] = from[i];
     }
 }
 
-template <int VPR, bool PAGED>       // 16-byte pieces of a row
-__global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
-    constexpr int kRows = kMove / VPR;
-    const int unit = blockIdx.x, ly = unit / (a.B * a.Hkv), b = (unit / a.Hkv) % a.B, h = unit % a.Hkv;
-    const int2 meta = a.meta[unit];
-    if (blockIdx.y == 0 && threadIdx.x == 0 && unit < a.B * a.Hkv && h == 0) a.new_len[b] = meta.y;
+// Rows i, i + step, .. of a unit's list move, by the threads of a workgroup: VPR 16-byte pieces of a row, K and V.
+template <int VPR, bool PAGED>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, int unit, int threads, int count, int part, int parts) {
+    constexpr int kBatch = 4;                // rows in flight
+    const int ly = unit / (a.B * a.Hkv), b = (unit / a.Hkv) % a.B, h = unit % a.Hkv;
     const int32_t* holes = a.lists + (size_t)unit * 2 * a.list_len;
     const int32_t* from = holes + a.list_len;
     const size_t row0 = (size_t)unit * a.S_cap;
-    const int piece = threadIdx.x % VPR;
+    const int piece = threadIdx.x % VPR, rows = threads / VPR;
     const size_t layer = PAGED ? (size_t)ly * a.num_pages * a.Hkv << a.page_shift : 0;
     const int32_t* table = a.block_table + (size_t)b * a.max_blocks;
     auto at = [&](int j) __attribute__((always_inline)) {
@@ -177,43 +75,329 @@ __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
         if constexpr (PAGED) row = layer + (((size_t)table[j >> a.page_shift] * a.Hkv + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
         return row * (VPR * 16) + piece * 16;
     };
-    for (int i = blockIdx.y * kRows + threadIdx.x / VPR; i < meta.x; i += gridDim.y * kRows) {
-        const int src = from[i], dst = holes[i];
-        const size_t s = at(src), d = at(dst);
-        const u32x4 k = *(const u32x4*)((const char*)a.k_cache + s), v = *(const u32x4*)((const char*)a.v_cache + s);
-        if (piece == 0) {
-            a.weight_out[row0 + dst] = a.weight[row0 + src];
-            a.key_pos_out[row0 + dst] = a.key_pos[row0 + src];
-            if (a.kept) a.kept[(size_t)unit * a.budget + dst] = src;
+    for (int i0 = part * rows * kBatch + threadIdx.x / VPR; i0 < count; i0 += parts * rows * kBatch) {
+        int src[kBatch], dst[kBatch];
+        size_t s[kBatch], d[kBatch];
+        u32x4 k[kBatch], v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = min(i0 + u * rows, count - 1);
+            src[u] = from[i];
+            dst[u] = holes[i];
         }
-        *(u32x4*)((char*)a.k_cache + d) = k;
-        *(u32x4*)((char*)a.v_cache + d) = v;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            s[u] = at(src[u]);
+            d[u] = at(dst[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            k[u] = *(const u32x4*)((const char*)a.k_cache + s[u]);
+            v[u] = *(const u32x4*)((const char*)a.v_cache + s[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u * rows >= count) continue;
+            if (piece == u) {                // (a lane of the row each, so that the batch's reads go out together)
+                a.weight_out[row0 + dst[u]] = a.weight[row0 + src[u]];
+                a.key_pos_out[row0 + dst[u]] = a.key_pos[row0 + src[u]];
+                if (a.kept) a.kept[(size_t)unit * a.budget + dst[u]] = src[u];
+            }
+            *(u32x4*)((char*)a.k_cache + d[u]) = k[u];
+            *(u32x4*)((char*)a.v_cache + d[u]) = v[u];
+        }
     }
 }
 
-template <int VPR>
-void move(const EvictArgs& a, hipStream_t st) {
-    const int units = a.layers * a.B * a.Hkv, rows = kMove / VPR;
+// VPR > 0: the workgroup moves its unit's rows too, and new_len is written here unless it is cache_len, which others may not have read.
+template <int WAVES, int VPR, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
+    constexpr int kThreads = WAVES * 64;
+    __shared__ uint32_t hist[3][kBins];
+    __shared__ uint32_t s_count[WAVES][4];
+    __shared__ uint32_t s_recent[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int unit = blockIdx.x, b = (unit / a.Hkv) % a.B;
+    const int n = a.cache_len[b];
+    bool bad = n < 0 || n > a.S_cap;
+    if constexpr (PAGED)
+        if (!bad)
+            for (int i = tid; i < (n + (1 << a.page_shift) - 1) >> a.page_shift; i += kThreads) {
+                const int id = a.block_table[(size_t)b * a.max_blocks + i];
+                bad = bad || id < 0 || id >= a.num_pages;
+            }
+    for (int i = tid; i < 3 * kBins; i += kThreads) ((uint32_t*)hist)[i] = 0;
+    bad = __syncthreads_or(bad) != 0;
+    const int m = min(n, a.budget);
+    const size_t row0 = (size_t)unit * a.S_cap;
+    const float* w = a.weight + row0;
+    const int32_t* pos = a.key_pos + row0;
+    int32_t* kept = a.kept ? a.kept + (size_t)unit * a.budget : nullptr;
+    if (unit < a.B * a.Hkv && unit % a.Hkv == 0 && tid == 0) {
+        if (a.status) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
+        if (VPR > 0 && a.new_len != a.cache_len) a.new_len[b] = bad ? n : m;
+    }
+    const bool apart = a.weight_out != a.weight, pos_apart = a.key_pos_out != a.key_pos;
+    if (bad || n <= a.budget) {
+        if (tid == 0) a.meta[unit] = make_int2(0, n);
+        if (kept)
+            for (int j = tid; j < a.budget; j += kThreads) kept[j] = !bad && j < n ? j : -1;
+        if (!bad)
+            for (int j = tid; j < n; j += kThreads) {
+                if (apart) a.weight_out[row0 + j] = w[j];
+                if (pos_apart) a.key_pos_out[row0 + j] = pos[j];
+            }
+        return;
+    }
+    const int newest = a.next_pos[b] - a.recent;
+
+    // ---- keys: a wave has a run of rows, 64 at a time
+    extern __shared__ uint32_t keys[];
+    const bool here = n <= a.lds_keys;
+    const int run = (n + kThreads - 1) / kThreads * 64, j0 = wave * run, j1 = min(n, j0 + run);
+    // f(j, key): of this wave's rows j .. j + 63, each lane its own; 0 for a row that does not exist
+    auto every = [&](auto f) __attribute__((always_inline)) {
+        if (here) {
+#pragma unroll 4
+            for (int jw = j0; jw < j1; jw += 64) f(jw, jw + lane < j1 ? keys[jw + lane] : 0u);
+        } else {
+#pragma unroll 4
+            for (int jw = j0; jw < j1; jw += 64) {
+                const int j = min(jw + lane, n - 1);
+                const uint32_t k = key_of(w[j], pos[j] >= newest);
+                f(jw, jw + lane < j1 ? k : 0u);
+            }
+        }
+    };
+    // The first look.  Eight rows of a lane in flight.
+    uint32_t recents = 0;
+    for (int jw = j0; jw < j1; jw += 512) {
+        float x[8];
+        int p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = min(jw + 64 * i + lane, n - 1);
+            x[i] = w[j];
+            p[i] = pos[j];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = jw + 64 * i + lane;
+            const bool on = j < j1, recent = p[i] >= newest;
+            const uint32_t k = key_of(x[i], recent);
+            recents += __popcll(__ballot(on && recent));
+            count<false>(hist[0], on && !recent, ~k >> 21);
+            if (on && here) keys[j] = k;
+        }
+    }
+    if (lane == 0) s_recent[wave] = recents;
+    // What lies before the budget is written as it is; movers come over it.
+    if (apart) copy_words<kThreads>((uint32_t*)a.weight_out + row0, (const uint32_t*)w, m);
+    if (pos_apart) copy_words<kThreads>((uint32_t*)a.key_pos_out + row0, (const uint32_t*)pos, m);
+    if (kept)
+        for (int j = tid; j < m; j += kThreads) kept[j] = j;
+    __syncthreads();
+
+    // ---- the m-th largest key, from its highest bits down; recent rows, which come first, were counted by themselves
+    uint32_t prefix = 0, left = (uint32_t)m;           // of the keys with these bits, `left` stay
+    uint32_t least = 0xFFFFFFFFu;                      // rows of larger keys stay, and the first `left` of this one
+    recents = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) recents += s_recent[i];
+    const bool others = recents < (uint32_t)m;         // some of them stay
+    if (others) left -= recents;
+    uint32_t in = 0;                                   // keys of the bin
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        if (!others) break;
+        const int bits = pass < 2 ? 11 : 10, lower = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        if (pass > 0) {
+            auto look = [&](auto crowded) __attribute__((always_inline)) {
+                every([&](int, uint32_t k) __attribute__((always_inline)) {
+                    count<decltype(crowded)::value>(hist[pass], k != 0xFFFFFFFFu && k >> ((lower + bits) & 31) == prefix && k != 0,
+                                                    (~k >> lower) & ((1u << bits) - 1u));
+                });
+            };
+            if (in * 8 > (uint32_t)n) look(std::integral_constant<bool, true>{});
+            else look(std::integral_constant<bool, false>{});
+            __syncthreads();
+        }
+        // lane l has bins 32 l .. of the digit's complement: larger keys first
+        uint32_t h[32], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) h[i] = hist[pass][bin_at(32 * lane + i)];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum += h[i];
+        uint32_t incl = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const uint32_t y = __shfl_up(incl, off);
+            if (lane >= off) incl += y;
+        }
+        uint32_t above = incl - sum, bin = 0, rest = 0, its = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if (above < left && left <= above + h[i]) { bin = i; rest = left - above; its = h[i]; }
+            above += h[i];
+        }
+        const int at = __ffsll((long long)__ballot(its != 0)) - 1;       // exactly one lane has it
+        const uint32_t digit = (uint32_t)(32 * at) + __builtin_amdgcn_readlane(bin, at);
+        left = __builtin_amdgcn_readlane(rest, at);
+        in = __builtin_amdgcn_readlane(its, at);
+        prefix = (prefix << bits) | (~digit & ((1u << bits) - 1u));
+        least = prefix << lower;
+        if (in == left) {                              // all of the bin
+            left = 0xFFFFFFFFu;
+            break;
+        }
+    }
+
+    // ---- the lists, in row order.  `left` equal rows stay; all of them where nothing was left over
+    int32_t* holes = a.lists + (size_t)unit * 2 * a.list_len;
+    int32_t* from = holes + a.list_len;
+    const unsigned long long below = (1ull << lane) - 1;
+    const bool tied = left != 0xFFFFFFFFu;
+    uint32_t same = 0, hole = 0, mover = 0, movers = 0;                // before this wave's rows; of the unit
+    if (here) {
+        // A wave lists its rows over the keys it has read, places first (rows before the budget come first); where its lists begin is known
+        // when all waves have theirs.
+        if (tied) {
+            uint32_t eq = 0;
+            every([&](int, uint32_t k) __attribute__((always_inline)) { eq += __popcll(__ballot(k == least)); });
+            if (lane == 0) s_count[wave][2] = eq;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) same += i < wave ? s_count[i][2] : 0u;
+        }
+        uint32_t mine = 0, my_holes = 0;
+        auto list = [&](auto tied_tag) __attribute__((always_inline)) {
+            every([&](int jw, uint32_t k) __attribute__((always_inline)) {
+                bool stays = k >= least;
+                if constexpr (decltype(tied_tag)::value) {
+                    const unsigned long long eq = __ballot(k == least);
+                    stays = k > least || (k == least && same + __popcll(eq & below) < left);
+                    same += __popcll(eq);
+                }
+                const unsigned long long st = __ballot(stays), front = m - jw >= 64 ? ~0ull : m > jw ? (1ull << (m - jw)) - 1 : 0ull;
+                const unsigned long long who = (st ^ front) & (j1 - jw >= 64 ? ~0ull : (1ull << (j1 - jw)) - 1);      // places, and movers
+                if ((who >> lane) & 1) keys[j0 + mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = jw + lane;
+                mine += __popcll(who);
+                my_holes += __popcll(who & front);
+            });
+        };
+        if (tied) list(std::integral_constant<bool, true>{});
+        else list(std::integral_constant<bool, false>{});
+        if (lane == 0) { s_count[wave][0] = my_holes; s_count[wave][1] = mine - my_holes; }
+        __syncthreads();
+        for (int i = 0; i < WAVES; ++i) {
+            if (i == wave) mover = movers;
+            if (i < wave) hole += s_count[i][0];
+            movers += s_count[i][1];
+        }
+        for (uint32_t i = lane; i < my_holes; i += 64) holes[hole + i] = keys[j0 + i];
+        for (uint32_t i = lane; i < mine - my_holes; i += 64) from[mover + i] = keys[j0 + my_holes + i];
+    } else {
+        // Longer units: counted first, then listed in place.
+        uint32_t more_front = 0, same_front = 0, more_back = 0, same_back = 0;
+        every([&](int jw, uint32_t k) __attribute__((always_inline)) {
+            const unsigned long long gt = __ballot(k > least), eq = __ballot(k == least), front = m - jw >= 64 ? ~0ull : m > jw ? (1ull << (m - jw)) - 1 : 0ull;
+            more_front += __popcll(gt & front); same_front += __popcll(eq & front);
+            more_back += __popcll(gt & ~front); same_back += __popcll(eq & ~front);
+        });
+        if (lane == 0) { s_count[wave][0] = more_front; s_count[wave][1] = same_front; s_count[wave][2] = more_back; s_count[wave][3] = same_back; }
+        __syncthreads();
+        uint32_t seen = 0;
+        for (int i = 0; i < WAVES; ++i) {
+            if (i == wave) { same = seen; mover = movers; }
+            const uint32_t keep_front = s_count[i][0] + min(s_count[i][1], left - min(left, seen));
+            seen += s_count[i][1];
+            const uint32_t keep_back = s_count[i][2] + min(s_count[i][3], left - min(left, seen));
+            seen += s_count[i][3];
+            if (i < wave) hole += (uint32_t)(min(m, (i + 1) * run) - min(m, i * run)) - keep_front;
+            movers += keep_back;
+        }
+        every([&](int jw, uint32_t k) __attribute__((always_inline)) {
+            const int j = jw + lane;
+            const unsigned long long eq = __ballot(k == least);
+            const bool stays = k > least || (k == least && same + __popcll(eq & below) < left);
+            same += __popcll(eq);
+            const bool is_hole = k != 0 && j < m && !stays, moves = j >= m && stays;
+            const unsigned long long bh = __ballot(is_hole), bm = __ballot(moves);
+            if (is_hole) holes[hole + __popcll(bh & below)] = j;
+            if (moves) from[mover + __popcll(bm & below)] = j;
+            hole += __popcll(bh);
+            mover += __popcll(bm);
+        });
+    }
+    if (tid == 0) a.meta[unit] = make_int2((int)movers, m);
+    if constexpr (VPR > 0) {
+        __syncthreads();
+        move_rows<VPR, PAGED>(a, unit, kThreads, (int)movers, 0, 1);
+    }
+}
+
+constexpr int kMove = 256;
+
+template <int VPR, bool PAGED>
+__global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
+    const int unit = blockIdx.x;
+    const int2 meta = a.meta[unit];
+    if (blockIdx.y == 0 && threadIdx.x == 0 && unit < a.B * a.Hkv && unit % a.Hkv == 0) a.new_len[(unit / a.Hkv) % a.B] = meta.y;
+    move_rows<VPR, PAGED>(a, unit, kMove, meta.x, blockIdx.y, gridDim.y);
+}
+
+// the lengths alone, where every workgroup has moved its unit's rows
+__global__ void evict_lengths_kernel(EvictArgs a) {
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < a.B) a.new_len[b] = a.meta[b * a.Hkv].y;
+}
+
+template <int WAVES, int VPR, bool PAGED>
+hipError_t select(EvictArgs a, int keys, hipStream_t st) {
+    static std::atomic<uint64_t> lds_set{0};
+    constexpr int kMost = (WAVES == 4 ? 8192 : kMostKeys) * 4;
+    const hipError_t e = ensure_dynamic_lds((const void*)evict_select_kernel<WAVES, VPR, PAGED>, kMost, lds_set);
+    if (e != hipSuccess) return e;
+    a.lds_keys = keys;
+    hipLaunchKernelGGL((evict_select_kernel<WAVES, VPR, PAGED>), dim3((unsigned)(a.layers * a.B * a.Hkv)), dim3(WAVES * 64), keys * 4, st, a);
+    return hipGetLastError();
+}
+
+template <int VPR, bool PAGED>
+hipError_t launch(const EvictArgs& a, hipStream_t st) {
+    const int units = a.layers * a.B * a.Hkv;
+    const int keys = a.S_cap < kMostKeys ? a.S_cap : kMostKeys;
+    const bool few = a.S_cap <= 8192;
+    // Where there are units enough to fill the chip, or next to nothing to move, who selects moves as well: other units are selected meanwhile.
+    const bool whole = few && (units >= 2 * a.cus || (long long)a.list_len * a.row_bytes <= 65536);
+    hipError_t e;
+    if (whole) {
+        e = select<4, VPR, PAGED>(a, keys, st);
+        if (e != hipSuccess || a.new_len != a.cache_len) return e;
+        hipLaunchKernelGGL(evict_lengths_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
+    e = few ? select<4, 0, PAGED>(a, keys, st) : select<16, 0, PAGED>(a, keys, st);
+    if (e != hipSuccess) return e;
+    const int rows = kMove / VPR * 4, most = (a.list_len + rows - 1) / rows;
     int runs = (8 * a.cus + units - 1) / units;
-    const int most = (a.list_len + rows - 1) / rows;
     if (runs > most) runs = most < 1 ? 1 : most;
-    const dim3 grid((unsigned)units, (unsigned)runs);
-    if (a.block_table) hipLaunchKernelGGL((evict_move_kernel<VPR, true>), grid, dim3(kMove), 0, st, a);
-    else hipLaunchKernelGGL((evict_move_kernel<VPR, false>), grid, dim3(kMove), 0, st, a);
+    hipLaunchKernelGGL((evict_move_kernel<VPR, PAGED>), dim3((unsigned)units, (unsigned)runs), dim3(kMove), 0, st, a);
+    return hipGetLastError();
+}
+template <int VPR>
+hipError_t launch(const EvictArgs& a, hipStream_t st) {
+    return a.block_table ? launch<VPR, true>(a, st) : launch<VPR, false>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(a.layers * a.B * a.Hkv)), dim3(kSelect), 0, st, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     switch (a.row_bytes / 16) {
-        case 8: move<8>(a, st); break;
-        case 16: move<16>(a, st); break;
-        default: move<32>(a, st); break;
+        case 8: return launch<8>(a, st);
+        case 16: return launch<16>(a, st);
+        default: return launch<32>(a, st);
     }
-    return hipGetLastError();
 }
 
 }  // namespace s4c

@@ -46,32 +46,24 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     const int n = a.cache_len[b], L = a.accept_len[b];
     const int32_t* path = a.path + (size_t)b * a.max_path;
 
-    // ---- is everything the sequence's?  (every workgroup finds the same)
-    bool bad = n < 1 || n > a.max_cache_len || n > a.S_cap || L < 0 || L >= a.max_path || L + 1 > n;
-    if (!bad) {
-        for (int k = tid; k <= L; k += kThreads) bad = bad || path[k] < 0 || path[k] >= a.N;
-        if constexpr (PAGED)
-            for (int i = tid; i < (n + (1 << a.page_shift) - 1) >> a.page_shift; i += kThreads) {
-                const int id = a.block_table[(size_t)b * a.max_blocks + i];
-                bad = bad || id < 0 || id >= a.num_pages;
-            }
+    const bool off_limits = n < 1 || n > a.max_cache_len || n > a.S_cap || L < 0 || L >= a.max_path || L + 1 > n;
+    if (off_limits) {
+        if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = S4C_SEQ_BAD_LEN;
+        return;
     }
-    bad = __syncthreads_or(bad) != 0;
-    if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
-    if (bad) return;
-
     const int first = n - (L + 1), R = (L + 1) * a.G, chunks = (R + kChunkRows - 1) / kChunkRows;
     // this workgroup's keys, in steps of all its waves' tiles
     constexpr int kStep = kWaves * T::kKeys;
     const int steps = (n + kStep - 1) / kStep, per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
     const int step0 = blockIdx.y * per, step1 = min(steps, step0 + per);
     if (step0 >= step1) return;
+    auto node_at = [&](int k) { return min(max(path[k], 0), a.N - 1); };        // (used before the path has been looked over)
 
     // query rows c kChunkRows .. into LDS
     auto stage = [&](int c) {
         const int r0 = c * kChunkRows, rows = min(kChunkRows, R - r0), up = (rows + 15) / 16 * 16;
         for (int r = tid; r < up; r += kThreads) {
-            const int k = min(r0 + r, R - 1) / a.G, g = min(r0 + r, R - 1) - k * a.G, node = path[k];
+            const int k = min(r0 + r, R - 1) / a.G, g = min(r0 + r, R - 1) - k * a.G, node = node_at(k);
             const size_t at = ((size_t)b * a.N + node) * a.Hq + kvh * a.G + g;
             s_node[r] = (int)k;
             s_lse[r] = r < rows ? a.lse[at] * kLog2e : INFINITY;
@@ -79,7 +71,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         }
         for (int e = tid; e < up * (T::kRowB / 16); e += kThreads) {
             const int r = e / (T::kRowB / 16), piece = e % (T::kRowB / 16);
-            const int rr = min(r0 + r, R - 1), k = rr / a.G, g = rr - k * a.G, node = path[k];
+            const int rr = min(r0 + r, R - 1), k = rr / a.G, g = rr - k * a.G, node = node_at(k);
             const uint4 v = *(const uint4*)((const unsigned char*)a.q + (((size_t)b * a.N + node) * a.Hq + kvh * a.G + g) * T::kRowB + piece * 16);
             *(uint4*)(s_q + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = v;
         }
@@ -95,7 +87,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         size_t row = row0 + j0;
         if constexpr (PAGED) {
             const int jc = min(j0, n - 1) & ~(T::kKeys - 1);
-            row = (((size_t)a.block_table[(size_t)b * a.max_blocks + (jc >> a.page_shift)] * a.Hkv + kvh) << a.page_shift) + (jc & ((1 << a.page_shift) - 1));
+            int id = a.block_table[(size_t)b * a.max_blocks + (jc >> a.page_shift)];
+            id = (unsigned)id < (unsigned)a.num_pages ? id : 0;
+            row = (((size_t)id * a.Hkv + kvh) << a.page_shift) + (jc & ((1 << a.page_shift) - 1));
         }
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -111,11 +105,20 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         w = a.weight_in[row0 + min(j0 + (lane & (T::kKeys - 1)), n - 1)];
     };
 
+    // The keys, the query rows and what tells whether they are the sequence's are requested together; every address is in bounds
+    // whatever the path and the table hold.
     fetch(step0, nf, npos, ntotal);
-    if (chunks == 1) {
-        stage(0);
-        __syncthreads();
-    }
+    bool bad = false;
+    for (int k = tid; k <= L; k += kThreads) bad = bad || path[k] < 0 || path[k] >= a.N;
+    if constexpr (PAGED)
+        for (int i = tid; i < (n + (1 << a.page_shift) - 1) >> a.page_shift; i += kThreads) {
+            const int id = a.block_table[(size_t)b * a.max_blocks + i];
+            bad = bad || id < 0 || id >= a.num_pages;
+        }
+    if (chunks == 1) stage(0);
+    bad = __syncthreads_or(bad) != 0;                                  // (every workgroup finds the same)
+    if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
+    if (bad) return;
     for (int step = step0; step < step1; ++step) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -153,12 +156,17 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
                 }
                 const int r4 = blk * 16 + 4 * (lane >> 4);
                 const f32x4 lse = *(const f32x4*)(s_lse + r4), slope = *(const f32x4*)(s_slope + r4);
-                score::change<NG>(s, a.score, a.scale_log2);
+                if (a.score.cap_log2 > 0.f) score::cap(s, a.score);
+                float off[NG][4];                                      // to the exponent
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) off[g][e] = -lse[e];
                 if (a.score.slopes) {
 #pragma unroll
                     for (int g = 0; g < NG; ++g)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[g][e] = fmaf(slope[e], rel[g], s[g][e]);
+                        for (int e = 0; e < 4; ++e) off[g][e] = fmaf(slope[e], rel[g], -lse[e]);
                 }
                 if (own_rows) {
 #pragma unroll
@@ -170,7 +178,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(s[g][e] - lse[e]);
+                    for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(fmaf(s[g][e], a.score.mul, off[g][e]));
             }
         }
         // lane 16 g + i has key 16 g + i of the tile
@@ -191,22 +199,28 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
 
 template <typename E, int D, int NG>
 hipError_t launch(const WeighArgs& a, hipStream_t st) {
-    const int units = a.B * a.Hkv, step = kWaves * 16 * NG;
-    const int steps = (a.max_cache_len + step - 1) / step;
-    int runs = (2 * 2 * a.cus + units - 1) / units;
-    if (runs > steps) runs = steps < 1 ? 1 : steps;
+    const int units = a.B * a.Hkv, step = kWaves * 16 * NG, steps = (a.max_cache_len + step - 1) / step;
+    int runs = (4 * a.cus + units - 1) / units;
+    if (runs > steps) runs = steps;
     const dim3 grid((unsigned)units, (unsigned)runs);
     if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true>), grid, dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false>), grid, dim3(kThreads), 0, st, a);
     return hipGetLastError();
 }
+// Tiles of half as many keys where whole ones would not be two workgroups for every CU.
+template <typename E, int D, int NG>
+hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
+    const long long step = kWaves * 16 * NG;
+    if ((long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step) < 2 * a.cus) return launch<E, D, NG / 2>(a, st);
+    return launch<E, D, NG>(a, st);
+}
 
 }  // namespace
 
 hipError_t launch_weigh(const WeighArgs& a, int dtype, hipStream_t st) {
-    if (dtype == S4C_F32) return a.D == 64 ? launch<float, 64, 4>(a, st) : launch<float, 128, 2>(a, st);
-    if (dtype == S4C_F16) return a.D == 64 ? launch<f16_t, 64, 4>(a, st) : launch<f16_t, 128, 4>(a, st);
-    return a.D == 64 ? launch<bf16_t, 64, 4>(a, st) : launch<bf16_t, 128, 4>(a, st);
+    if (dtype == S4C_F32) return a.D == 64 ? launch_tiles<float, 64, 4>(a, st) : launch_tiles<float, 128, 2>(a, st);
+    if (dtype == S4C_F16) return a.D == 64 ? launch_tiles<f16_t, 64, 4>(a, st) : launch_tiles<f16_t, 128, 4>(a, st);
+    return a.D == 64 ? launch_tiles<bf16_t, 64, 4>(a, st) : launch_tiles<bf16_t, 128, 4>(a, st);
 }
 
 }  // namespace s4c

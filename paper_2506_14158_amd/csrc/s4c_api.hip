@@ -760,15 +760,30 @@ bool is_finite(float x) {
     return (u & 0x7F800000u) != 0x7F800000u;
 }
 // How the scores of a call with this scale are changed; false: not a score that the kernels take.
-bool score_args(const s4c_score* sc, float scale, int32_t D, score::Args<score::kChanged>* a, s4c_status* why) {
+bool score_args(const s4c_score* sc, float scale, int32_t D, score::Changed* a, s4c_status* why) {
     *a = {};
+    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
+    a->mul = scale * kLog2e;
+    a->slope_mul = kLog2e / a->mul;
     if (!sc) return true;
     if (sc->key_pos && !sc->root_pos) { *why = S4C_ERR_NULL; return false; }
     if (!is_finite(sc->cap) || sc->cap < 0.f) { *why = S4C_ERR_SHAPE; return false; }
     if (sc->cap > 0.f) {
         a->cap_log2 = sc->cap * kLog2e;
-        a->to_y = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) / sc->cap;
+        a->to_y = scale / sc->cap;
         if (!is_finite(2.f * a->cap_log2) || !is_finite(a->to_y)) { *why = S4C_ERR_SHAPE; return false; }
+        a->mul = 1.f;
+        a->slope_mul = kLog2e;
+        // (where a coefficient leaves fp32's normal numbers, the fit that takes y does)
+        constexpr double kFour[4] = {0.999999965, -0.333324202, 0.132957516, -0.0489556371};
+        const double y2 = (double)a->to_y * a->to_y;
+        double c = (double)a->cap_log2 * a->to_y;
+        bool normal = true;
+        for (int i = 0; i < 4; ++i, c *= y2) {
+            a->fit[i] = (float)(kFour[i] * c);
+            normal = normal && fabs(kFour[i] * c) > 1e-37 && fabs(kFour[i] * c) < 1e37;
+        }
+        a->fit_up_to = normal ? 0.35f / a->to_y : 0.f;
     }
     a->slopes = sc->slopes;
     a->key_pos = sc->key_pos;
@@ -785,7 +800,7 @@ s4c_status tree_attn_scored_impl(const s4c_attn_shape* shape, const s4c_score* s
     const s4c_status ok = tree_attn_prepare(shape, q, k_tree, v_tree, k_cache, v_cache, block_table, max_blocks, page_shift, num_pages,
                                             cache_len, parent, max_cache_len, scale, out, status, workspace, workspace_bytes, &p, &a);
     if (ok != S4C_OK) return ok;
-    score::Args<score::kChanged> sc;
+    score::Changed sc;
     s4c_status why;
     if (!score_args(score_in, scale, shape->D, &sc, &why)) return why;
     if (!sc.slopes) sc.key_pos = sc.root_pos = nullptr;       // nothing depends on positions
@@ -810,7 +825,6 @@ s4c_status weigh_impl(const s4c_attn_shape* shape, const s4c_score* score_in, co
     if (!score_args(score_in, scale, shape->D, &a.score, &why)) return why;
     a.q = q; a.k_cache = k_cache; a.lse = lse; a.cache_len = cache_len; a.path = path; a.accept_len = accept_len;
     a.weight_in = weight_in; a.weight = weight; a.key_pos = score_in ? score_in->key_pos : nullptr; a.status = status;
-    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)shape->D)) * kLog2e;
     a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.D = shape->D; a.N = shape->N; a.S_cap = shape->S_cap;
     a.G = shape->Hq / shape->Hkv; a.max_path = max_path; a.max_cache_len = max_cache_len; a.cus = device_cus();
     a.block_table = block_table; a.max_blocks = max_blocks; a.page_shift = page_shift; a.num_pages = num_pages;

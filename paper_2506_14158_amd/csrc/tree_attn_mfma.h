@@ -45,7 +45,7 @@ constexpr int scored_lds_bytes_for(int ns, int d, int wr) { return lds_bytes_for
 template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
-    constexpr bool kScored = SCORE == score::kChanged;
+    constexpr bool kScored = SCORE != score::kPlain;
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row
@@ -281,9 +281,9 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     if constexpr (STEP != kNoStep) lens_read(tail, a, lens);
     while (issued < NS - 1 && issued < n_share) issue_next();
 
-    float slope = 0.f;                                    // of this lane's row, in log2 units
+    float slope = 0.f;                                    // of this lane's row, in units of the scores before sc.mul
     if constexpr (kScored)
-        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * kLog2e;
+        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * sc.slope_mul;
     int parent = -1, b_known = cw.b;
     bool masks = false;                                   // anc[] holds b_known's masks
     while (cw.b >= 0) {
@@ -368,18 +368,41 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);      // 8 MFMAs
         }
 
+        // ---- changed scores
+        float mul = a.scale_log2, off = 0.f;                  // to log2 units
+        bool fits = false;
         if constexpr (kScored) {
+            mul = sc.mul;
+            auto add_positions = [&]() __attribute__((always_inline)) {
+                if constexpr (MODE == kTree) score::add_depths(s, slope, depths + arg * kBN + 4 * g32);
+                else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + ((uint32_t)done % NS) * kBN + 4 * g32, root);
+                else off = score::add_rows(s, slope, key0 + 4 * g32 - P, sc);
+            };
+            if constexpr (SCORE == score::kSlopes) add_positions();
+            if constexpr (SCORE == score::kCap || SCORE == score::kCapSlopes) {
+                if constexpr (MODE == kPlain) {
+                    float most = fmaxf(fabsf(s[0][0]), fabsf(s[1][0]));
 #pragma unroll
-            for (int kblk = 0; kblk < 2; ++kblk) {
-                score::change(s[kblk], sc, a.scale_log2);
-                if (sc.slopes) {
-                    if constexpr (MODE == kTree) score::add_depths(s[kblk], slope, depths + arg * kBN + 32 * kblk + 4 * g32);
-                    else if (sc.key_pos) score::add_looked_up(s[kblk], slope, ring_pos + ((uint32_t)done % NS) * kBN + 32 * kblk + 4 * g32, root);
-                    else score::add_rows(s[kblk], slope, key0 + 32 * kblk + 4 * g32 - P);
+                    for (int j = 1; j < 16; ++j) most = __builtin_fmaxf(__builtin_fmaxf(most, fabsf(s[0][j])), fabsf(s[1][j]));
+                    fits = !__any(most > sc.fit_up_to);
+                }
+                if (MODE != kPlain || __builtin_expect(!fits, 0)) {
+                    score::cap(s[0], sc);
+                    score::cap(s[1], sc);
                 }
             }
+            if constexpr (SCORE == score::kCapSlopes) {
+                if constexpr (MODE == kPlain) {
+                    const score::Factor<true> capped(sc, fits, 1.f);
+#pragma unroll
+                    for (int kblk = 0; kblk < 2; ++kblk)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) s[kblk][j] *= capped(s[kblk][j]);
+                }
+                add_positions();
+            }
         }
-        const float to_log2 = kScored ? 1.f : a.scale_log2;
+        const score::Factor<SCORE == score::kCap && MODE == kPlain> factor(sc, fits, mul);
         // key of register j of block kblk, relative to the tile: 32 kblk + 8 (j/4) + 4 g32 + (j%4)
         if constexpr (MODE == kTree) {
             const int w0 = arg * 2;                     // 32-node word of block 0
@@ -403,6 +426,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int j = 1; j < 16; ++j) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[0][j]), s[1][j]);    // v_max3_f32
+        if constexpr (kScored) mx = fmaf(mx, factor(mx), off);        // (tanh grows with its argument; the halves have different keys: before they meet)
         mx = max_across_halves(mx);
         float psum = 0.f;
         if constexpr (MODE == kPlain) {
@@ -412,7 +436,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             // 64 multiplications of the output accumulator are skipped.  Sum and accumulator stay
             // consistent with whatever reference is current, which is all the final division (or the
             // merge of KV splits) needs.
-            const float mt = mx * to_log2;
+            const float mt = kScored ? mx : mx * mul;
             if (__any(mt > m_run + kLazyLog2)) {
                 const float m_new = fmaxf(m_run, mt);
                 const float alpha = fast_exp2(m_run - m_new);          // first tile: exp2(-inf) = 0
@@ -427,13 +451,13 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], to_log2, kShift - m_run));
+                    const float p = fast_exp2(fmaf(s[kblk][j], factor(s[kblk][j]), kScored ? off + (kShift - m_run) : kShift - m_run));
                     s[kblk][j] = p;
                     psum += p;
                 }
             l_run += psum;
         } else {
-            const float m_new = fmaxf(m_run, mx * to_log2);
+            const float m_new = fmaxf(m_run, kScored ? mx : mx * mul);
             float m_safe = m_new;
             if constexpr (MODE == kTree) m_safe = (m_new == -INFINITY) ? 0.f : m_new;   // row with no visible key yet
             const float alpha = fast_exp2(m_run - m_safe);
@@ -441,7 +465,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], to_log2, kShift - m_safe));
+                    const float p = fast_exp2(fmaf(s[kblk][j], mul, kScored ? off + (kShift - m_safe) : kShift - m_safe));
                     s[kblk][j] = p;
                     psum += p;
                 }
@@ -549,7 +573,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             if (nw.b != b && tid < N) parent = a.parent[(size_t)nw.b * N + tid];
             load_q(nw.b, nw.kvh);
             if constexpr (kScored)
-                if (sc.slopes) slope = sc.slopes[nw.kvh * G + g] * kLog2e;
+                if (sc.slopes) slope = sc.slopes[nw.kvh * G + g] * sc.slope_mul;
         }
         if (mt == 0 && tid == 0) work::note_parts(a, team, cw);
     }
@@ -641,23 +665,23 @@ hipError_t launch_rows(const AttnArgs& a, const StepTail<STEP>& tail, hipStream_
         if (a.tag == 0) return launch_rows<PAGED, F16, D, STEP, parts::kNext>(a, tail, st);
     return launch_rows<PAGED, F16, D, STEP, parts::kHere>(a, tail, st);
 }
-// ... of attention with changed scores
-template <bool PAGED, bool F16, int D, parts::Merge MERGE>
-hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+// ... of attention with changed scores, one kind in a translation unit
+template <bool PAGED, bool F16, int D, parts::Merge MERGE, score::Kind SCORE>
+hipError_t launch_scored(const AttnArgs& a, const score::Changed& sc, hipStream_t st) {
     const StepTail<kNoStep> none;
-    return pick_wr(a.M) == 4 ? launch<4, 4, D == 64 ? 2 : 1, PAGED, F16, D, kNoStep, MERGE, score::kChanged>(a, none, st, sc)
-                             : launch<8, 4, 2, PAGED, F16, D, kNoStep, MERGE, score::kChanged>(a, none, st, sc);
+    return pick_wr(a.M) == 4 ? launch<4, 4, D == 64 ? 2 : 1, PAGED, F16, D, kNoStep, MERGE, SCORE>(a, none, st, sc)
+                             : launch<8, 4, 2, PAGED, F16, D, kNoStep, MERGE, SCORE>(a, none, st, sc);
 }
-template <bool PAGED, bool F16, int D>
-hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
-    return a.split == 1   ? launch_scored<PAGED, F16, D, parts::kWhole>(a, sc, st)
-           : a.split == 0 ? launch_scored<PAGED, F16, D, parts::kShares>(a, sc, st)
-                          : launch_scored<PAGED, F16, D, parts::kHere>(a, sc, st);
+template <bool PAGED, bool F16, int D, score::Kind SCORE>
+hipError_t launch_scored(const AttnArgs& a, const score::Changed& sc, hipStream_t st) {
+    return a.split == 1   ? launch_scored<PAGED, F16, D, parts::kWhole, SCORE>(a, sc, st)
+           : a.split == 0 ? launch_scored<PAGED, F16, D, parts::kShares, SCORE>(a, sc, st)
+                          : launch_scored<PAGED, F16, D, parts::kHere, SCORE>(a, sc, st);
 }
-template <bool F16>
-hipError_t launch_large_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
-    if (a.D == 64) return a.block_table ? launch_scored<true, F16, 64>(a, sc, st) : launch_scored<false, F16, 64>(a, sc, st);
-    return a.block_table ? launch_scored<true, F16, 128>(a, sc, st) : launch_scored<false, F16, 128>(a, sc, st);
+template <bool F16, score::Kind SCORE>
+hipError_t launch_large_scored(const AttnArgs& a, const score::Changed& sc, hipStream_t st) {
+    if (a.D == 64) return a.block_table ? launch_scored<true, F16, 64, SCORE>(a, sc, st) : launch_scored<false, F16, 64, SCORE>(a, sc, st);
+    return a.block_table ? launch_scored<true, F16, 128, SCORE>(a, sc, st) : launch_scored<false, F16, 128, SCORE>(a, sc, st);
 }
 template <bool F16, int D>
 hipError_t launch_as(const AttnArgs& a, const StepTail<kGreedyStep>* step, hipStream_t st) {

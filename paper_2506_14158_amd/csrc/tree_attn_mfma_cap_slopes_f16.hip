@@ -1,0 +1,8 @@
+// tree_attn_mfma.h for fp16 data, with capped scores and slopes over the keys' positions.
+#include "tree_attn_mfma.h"
+
+namespace s4c {
+
+hipError_t launch_large_cap_slopes_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st) { return launch_large_scored<true, score::kCapSlopes>(a, sc, st); }
+
+}  // namespace s4c

@@ -84,7 +84,7 @@ struct Cfg {
 template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kPerCu * C::kWaves / 4, 2)))
 void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
-    constexpr bool kScored = SCORE == score::kChanged;
+    constexpr bool kScored = SCORE != score::kPlain;
     constexpr int kD = C::kD, kKG = C::kKG, kRBW = C::kRBW, kNR = C::kNR, kRowB = C::kRowB;
     constexpr int kThreads = C::kThreads, kCH = C::kCH;
     constexpr bool kIs32 = C::kElem == kF32, F16 = C::kElem == kH16;
@@ -318,9 +318,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
             if (rvalid) qf[t] = *(const uint4*)(qrow + 32 * t);
         }
     };
-    float slope = 0.f;                                        // of this lane's row, in log2 units
+    float slope = 0.f;                                        // of this lane's row, in units of the scores before sc.mul
     if constexpr (kScored)
-        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * kLog2e;
+        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * sc.slope_mul;
     int parent = -1, b_known = cw.b;
     bool masks = false;                                       // anc[] holds b_known's masks
     while (cw.b >= 0) {
@@ -401,16 +401,17 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s[j] += s1[j];
             }
-            constexpr bool kLog2Units = kScored;              // of s from here on
+            float mul = a.scale_log2, off = 0.f;              // to log2 units
             if constexpr (kScored) {
-                score::change(s, sc, a.scale_log2);
+                mul = sc.mul;
+                if (sc.cap_log2 > 0.f) score::cap(s, sc);
                 if (sc.slopes) {
-                    if (MASKED && my >= u_pref) score::add_depths(s, slope, depths + (my - u_pref) * kBN + 4 * g32);
-                    else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);
-                    else score::add_rows(s, slope, my * kBN + 4 * g32 - P);
+                    f32x16(&one)[1] = reinterpret_cast<f32x16(&)[1]>(s);
+                    if (MASKED && my >= u_pref) score::add_depths(one, slope, depths + (my - u_pref) * kBN + 4 * g32);
+                    else if (sc.key_pos) score::add_looked_up(one, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);
+                    else off = score::add_rows(one, slope, my * kBN + 4 * g32 - P, sc);
                 }
             }
-            const float to_log2 = kLog2Units ? 1.f : a.scale_log2;
             if constexpr (MASKED) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
@@ -419,7 +420,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
             float mx = s[0];
 #pragma unroll
             for (int j = 1; j < 16; j += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[j]), s[(j + 1) & 15]);
-            mx = max_across_halves(mx) * to_log2;
+            // (the two halves of a row have different keys: what is added goes first)
+            if constexpr (kScored) mx = max_across_halves(fmaf(mx, mul, off));
+            else mx = max_across_halves(mx) * mul;
             // The reference moves only when some row of the wave outgrew it by more than 2^kLag (always at its first
             // visible key); until then the accumulator is not touched.
             if (__any(mx > m_run + kLag)) {
@@ -438,7 +441,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
             float psum = 0.f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float p = fast_exp2(fmaf(s[j], to_log2, kShift - m_ref));
+                const float p = fast_exp2(fmaf(s[j], mul, kScored ? off + (kShift - m_ref) : kShift - m_ref));
                 s[j] = p;
                 psum += p;
             }
@@ -516,7 +519,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
                 if (nw.b != b && tid < N) parent = a.parent[(size_t)nw.b * N + tid];
                 load_q(nw.b, nw.kvh);
                 if constexpr (kScored)
-                    if (sc.slopes) slope = sc.slopes[nw.kvh * G + gh] * kLog2e;
+                    if (sc.slopes) slope = sc.slopes[nw.kvh * G + gh] * sc.slope_mul;
             }
         }
         const int flagged = (work::tree_is_bad(a, spar) ? S4C_SEQ_BAD_TREE : 0) | (len_bad ? S4C_SEQ_BAD_LEN : 0);
@@ -669,14 +672,14 @@ auto with_cfg(int D, int rows, Use use) {
 }
 // ... of attention with changed scores
 template <class C, bool PAGED>
-hipError_t launch_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+hipError_t launch_scored(const AttnArgs& a, const score::Changed& sc, hipStream_t st) {
     const StepTail<kNoStep> none;
-    if (a.split == 1) return launch<C, PAGED, kNoStep, parts::kWhole, score::kChanged>(a, none, st, sc);
-    if (a.split == 0) return launch<C, PAGED, kNoStep, parts::kShares, score::kChanged>(a, none, st, sc);
-    return launch<C, PAGED, kNoStep, parts::kHere, score::kChanged>(a, none, st, sc);
+    if (a.split == 1) return launch<C, PAGED, kNoStep, parts::kWhole, score::kAny>(a, none, st, sc);
+    if (a.split == 0) return launch<C, PAGED, kNoStep, parts::kShares, score::kAny>(a, none, st, sc);
+    return launch<C, PAGED, kNoStep, parts::kHere, score::kAny>(a, none, st, sc);
 }
 template <Elem E>
-hipError_t launch_smallm_scored(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) {
+hipError_t launch_smallm_scored(const AttnArgs& a, const score::Changed& sc, hipStream_t st) {
     return with_cfg<E>(a.D, a.tile_rows, [&](auto c) {
         typedef decltype(c) C;
         return a.block_table ? launch_scored<C, true>(a, sc, st) : launch_scored<C, false>(a, sc, st);

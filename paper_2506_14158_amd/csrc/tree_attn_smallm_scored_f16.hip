@@ -3,6 +3,6 @@
 
 namespace s4c {
 
-hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Args<score::kChanged>& sc, hipStream_t st) { return launch_smallm_scored<kH16>(a, sc, st); }
+hipError_t launch_smallm_scored_f16(const AttnArgs& a, const score::Changed& sc, hipStream_t st) { return launch_smallm_scored<kH16>(a, sc, st); }
 
 }  // namespace s4c

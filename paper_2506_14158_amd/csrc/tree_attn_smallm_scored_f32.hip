@@ -3,7 +3,7 @@
 
 namespace s4c {
 
-hipError_t launch_tree_attn_small_scored(const AttnArgs& a, int dtype, const score::Args<score::kChanged>& sc, hipStream_t st) {
+hipError_t launch_tree_attn_small_scored(const AttnArgs& a, int dtype, const score::Changed& sc, hipStream_t st) {
     return dtype == S4C_F32   ? launch_smallm_scored<kF32>(a, sc, st)
            : dtype == S4C_F16 ? launch_smallm_scored_f16(a, sc, st)
                               : launch_smallm_scored_bf16(a, sc, st);

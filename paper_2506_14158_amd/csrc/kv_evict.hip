@@ -21,15 +21,26 @@ constexpr int kBins = 2048;
 constexpr int kMostKeys = 32768;             // in LDS
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// a total's bits in the order of the numbers, 1 .. 2^32 - 2 (-0 as 0); recent rows: 2^32 - 1; 0 is no row's
+// A total's bits in the order of the numbers, 2^21 .. 2^32 - 2 (-0 as 0); recent rows: 2^32 - 1.  So the first digit of a key is never 0, nor is the smallest
+// that stays, whatever the totals hold: 0 stands for rows that do not exist.
 __device__ __forceinline__ uint32_t key_of(float w, bool recent) {
     const uint32_t u = __float_as_uint(w + 0.f);
     const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-    return recent ? 0xFFFFFFFFu : min(max(k, 1u), 0xFFFFFFFEu);
+    return recent ? 0xFFFFFFFFu : min(max(k, 1u << 21), 0xFFFFFFFEu);
 }
 
 // Where bin d of a histogram lies: a scanning lane l reads bins 32 l .. 32 l + 31, each time all lanes from different banks.
 __device__ __forceinline__ uint32_t bin_at(uint32_t d) { return d ^ (d >> 5); }
+
+__device__ __forceinline__ uint32_t wave_inclusive(uint32_t x) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t y = __shfl_up(x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
 
 // One more in bin d for every lane that is `on`.  Lanes that add to one word wait for each other; CROWDED, where most keys may share a bin, one lane
 // adds for all if all agree.
@@ -110,6 +121,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int unit, int thre
 }
 
 // VPR > 0: the workgroup moves its unit's rows too, and new_len is written here unless it is cache_len, which others may not have read.
+// Otherwise a second one for every unit (blockIdx.y) writes what lies before the budget as it is; movers come over it.
 template <int WAVES, int VPR, bool PAGED>
 __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
     constexpr int kThreads = WAVES * 64;
@@ -133,11 +145,21 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
     const float* w = a.weight + row0;
     const int32_t* pos = a.key_pos + row0;
     int32_t* kept = a.kept ? a.kept + (size_t)unit * a.budget : nullptr;
-    if (unit < a.B * a.Hkv && unit % a.Hkv == 0 && tid == 0) {
+    if (unit < a.B * a.Hkv && unit % a.Hkv == 0 && tid == 0 && blockIdx.y == 0) {
         if (a.status) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
         if (VPR > 0 && a.new_len != a.cache_len) a.new_len[b] = bad ? n : m;
     }
     const bool apart = a.weight_out != a.weight, pos_apart = a.key_pos_out != a.key_pos;
+    auto write_front = [&]() __attribute__((always_inline)) {
+        if (apart) copy_words<kThreads>((uint32_t*)a.weight_out + row0, (const uint32_t*)w, m);
+        if (pos_apart) copy_words<kThreads>((uint32_t*)a.key_pos_out + row0, (const uint32_t*)pos, m);
+        if (kept)
+            for (int j = tid; j < m; j += kThreads) kept[j] = j;
+    };
+    if (VPR == 0 && blockIdx.y > 0) {
+        if (!bad && n > a.budget) write_front();
+        return;
+    }
     if (bad || n <= a.budget) {
         if (tid == 0) a.meta[unit] = make_int2(0, n);
         if (kept)
@@ -169,19 +191,20 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
             }
         }
     };
-    // The first look.  Eight rows of a lane in flight.
+    // The first look.  Every load of a turn is in flight at once.
+    constexpr int kLook = WAVES == 16 ? 16 : 8;
     uint32_t recents = 0;
-    for (int jw = j0; jw < j1; jw += 512) {
-        float x[8];
-        int p[8];
+    for (int jw = j0; jw < j1; jw += 64 * kLook) {
+        float x[kLook];
+        int p[kLook];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kLook; ++i) {
             const int j = min(jw + 64 * i + lane, n - 1);
             x[i] = w[j];
             p[i] = pos[j];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kLook; ++i) {
             const int j = jw + 64 * i + lane;
             const bool on = j < j1, recent = p[i] >= newest;
             const uint32_t k = key_of(x[i], recent);
@@ -191,11 +214,7 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
         }
     }
     if (lane == 0) s_recent[wave] = recents;
-    // What lies before the budget is written as it is; movers come over it.
-    if (apart) copy_words<kThreads>((uint32_t*)a.weight_out + row0, (const uint32_t*)w, m);
-    if (pos_apart) copy_words<kThreads>((uint32_t*)a.key_pos_out + row0, (const uint32_t*)pos, m);
-    if (kept)
-        for (int j = tid; j < m; j += kThreads) kept[j] = j;
+    if constexpr (VPR > 0) write_front();
     __syncthreads();
 
     // ---- the m-th largest key, from its highest bits down; recent rows, which come first, were counted by themselves
@@ -222,28 +241,19 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
             else look(std::integral_constant<bool, false>{});
             __syncthreads();
         }
-        // lane l has bins 32 l .. of the digit's complement: larger keys first
-        uint32_t h[32], sum = 0;
+        // lane l has bins 32 l .. of the digit's complement, larger keys first: which lane's, then which of them
+        uint32_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) h[i] = hist[pass][bin_at(32 * lane + i)];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) sum += h[i];
-        uint32_t incl = sum;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t y = __shfl_up(incl, off);
-            if (lane >= off) incl += y;
-        }
-        uint32_t above = incl - sum, bin = 0, rest = 0, its = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            if (above < left && left <= above + h[i]) { bin = i; rest = left - above; its = h[i]; }
-            above += h[i];
-        }
-        const int at = __ffsll((long long)__ballot(its != 0)) - 1;       // exactly one lane has it
-        const uint32_t digit = (uint32_t)(32 * at) + __builtin_amdgcn_readlane(bin, at);
-        left = __builtin_amdgcn_readlane(rest, at);
-        in = __builtin_amdgcn_readlane(its, at);
+        for (int i = 0; i < 32; ++i) sum += hist[pass][bin_at(32 * lane + i)];
+        uint32_t incl = wave_inclusive(sum);
+        const int at = __ffsll((long long)__ballot(incl >= left)) - 1;
+        left -= __builtin_amdgcn_readlane(incl - sum, at);
+        sum = lane < 32 ? hist[pass][bin_at(32 * at + lane)] : 0u;
+        incl = wave_inclusive(sum);
+        const int bin = __ffsll((long long)__ballot(incl >= left)) - 1;
+        left -= __builtin_amdgcn_readlane(incl - sum, bin);
+        in = __builtin_amdgcn_readlane(sum, bin);
+        const uint32_t digit = (uint32_t)(32 * at + bin);
         prefix = (prefix << bits) | (~digit & ((1u << bits) - 1u));
         least = prefix << lower;
         if (in == left) {                              // all of the bin
@@ -270,25 +280,34 @@ __global__ __launch_bounds__(WAVES * 64) void evict_select_kernel(EvictArgs a) {
             for (int i = 0; i < WAVES; ++i) same += i < wave ? s_count[i][2] : 0u;
         }
         uint32_t mine = 0, my_holes = 0;
-        auto list = [&](auto tied_tag) __attribute__((always_inline)) {
-            every([&](int jw, uint32_t k) __attribute__((always_inline)) {
-                bool stays = k >= least;
-                if constexpr (decltype(tied_tag)::value) {
-                    const unsigned long long eq = __ballot(k == least);
-                    stays = k > least || (k == least && same + __popcll(eq & below) < left);
-                    same += __popcll(eq);
-                }
-                const unsigned long long st = __ballot(stays), front = m - jw >= 64 ? ~0ull : m > jw ? (1ull << (m - jw)) - 1 : 0ull;
-                const unsigned long long who = (st ^ front) & (j1 - jw >= 64 ? ~0ull : (1ull << (j1 - jw)) - 1);      // places, and movers
-                if ((who >> lane) & 1) keys[j0 + mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = jw + lane;
-                mine += __popcll(who);
-                my_holes += __popcll(who & front);
-            });
+        auto note = [&](unsigned long long who, int jw) __attribute__((always_inline)) {
+            if ((who >> lane) & 1) keys[j0 + mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = jw + lane;
+            mine += __popcll(who);
         };
-        if (tied) list(std::integral_constant<bool, true>{});
-        else list(std::integral_constant<bool, false>{});
+        auto stays = [&](uint32_t k) __attribute__((always_inline)) {
+            if (!tied) return __ballot(k >= least);
+            const unsigned long long eq = __ballot(k == least);
+            const bool s = k > least || (k == least && same + __popcll(eq & below) < left);
+            same += __popcll(eq);
+            return __ballot(s);
+        };
+        int jw = j0;
+#pragma unroll 4
+        for (const int e = min(j1, m) - 63; jw < e; jw += 64) note(~stays(keys[jw + lane]), jw);
+        if (jw < min(j1, m)) {                         // the rows on both sides of the budget
+            const unsigned long long st = stays(jw + lane < j1 ? keys[jw + lane] : 0u), front = (1ull << (m - jw)) - 1;
+            note(~st & front, jw);
+            my_holes = mine;
+            note(st & ~front, jw);
+            jw += 64;
+        } else {
+            my_holes = mine;
+        }
+#pragma unroll 4
+        for (; jw < j1; jw += 64) note(stays(jw + lane < j1 ? keys[jw + lane] : 0u), jw);
         if (lane == 0) { s_count[wave][0] = my_holes; s_count[wave][1] = mine - my_holes; }
         __syncthreads();
+#pragma unroll
         for (int i = 0; i < WAVES; ++i) {
             if (i == wave) mover = movers;
             if (i < wave) hole += s_count[i][0];
@@ -359,7 +378,9 @@ hipError_t select(EvictArgs a, int keys, hipStream_t st) {
     const hipError_t e = ensure_dynamic_lds((const void*)evict_select_kernel<WAVES, VPR, PAGED>, kMost, lds_set);
     if (e != hipSuccess) return e;
     a.lds_keys = keys;
-    hipLaunchKernelGGL((evict_select_kernel<WAVES, VPR, PAGED>), dim3((unsigned)(a.layers * a.B * a.Hkv)), dim3(WAVES * 64), keys * 4, st, a);
+    const bool front = VPR == 0 && (a.kept || a.weight_out != a.weight || a.key_pos_out != a.key_pos);
+    const dim3 grid((unsigned)(a.layers * a.B * a.Hkv), front ? 2u : 1u);
+    hipLaunchKernelGGL((evict_select_kernel<WAVES, VPR, PAGED>), grid, dim3(WAVES * 64), keys * 4, st, a);
     return hipGetLastError();
 }
 

@@ -15,12 +15,11 @@ namespace {
 using namespace mfma;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kChunkRows = 128;              // query rows in LDS at a time
-
 // 16-byte pieces of a row that a lane has: piece 4 t + lane / 16 of its row for t < T.
 template <typename E, int D, int NG>
 struct Tile {
     static constexpr int kRowB = D * sizeof(E), kT = kRowB / 64, kKeys = 16 * NG;
+    static constexpr int kRows = kRowB == 512 ? 64 : 128;        // query rows in LDS at a time
 };
 
 template <typename E>
@@ -35,12 +34,16 @@ __device__ __forceinline__ f32x4 product(uint4 q, uint4 k, f32x4 c) {
     }
 }
 
-template <typename E, int D, int NG, bool PAGED>
+// MANY: the path may have more query rows than lie in LDS at a time.  Then these are replaced while the matrix cores work, chunk by chunk for
+// every tile of keys (two buffers, one barrier a chunk).
+template <typename E, int D, int NG, bool PAGED, bool MANY>
 __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     typedef Tile<E, D, NG> T;
-    __shared__ __attribute__((aligned(16))) unsigned char s_q[kChunkRows * T::kRowB];     // [16-row block][piece t][lane] 16 bytes
-    __shared__ __attribute__((aligned(16))) float s_lse[kChunkRows], s_slope[kChunkRows];
-    __shared__ int s_node[kChunkRows];
+    constexpr int kBufs = MANY ? 2 : 1, kTogether = MANY ? 2 : 1;       // blocks of 16 rows at a time
+    __shared__ __attribute__((aligned(16))) unsigned char s_q[kBufs][T::kRows * T::kRowB];     // [16-row block][piece t][lane] 16 bytes
+    __shared__ __attribute__((aligned(16))) float s_lse[kBufs][T::kRows], s_slope[kBufs][T::kRows];
+    __shared__ int s_node[kBufs][T::kRows];
+    __shared__ int s_path[kMaxNodes];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int unit = blockIdx.x, b = unit / a.Hkv, kvh = unit - b * a.Hkv;
     const int n = a.cache_len[b], L = a.accept_len[b];
@@ -51,30 +54,57 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = S4C_SEQ_BAD_LEN;
         return;
     }
-    const int first = n - (L + 1), R = (L + 1) * a.G, chunks = (R + kChunkRows - 1) / kChunkRows;
+    const int first = n - (L + 1), R = (L + 1) * a.G, chunks = MANY ? (R + T::kRows - 1) / T::kRows : 1;
     // this workgroup's keys, in steps of all its waves' tiles
     constexpr int kStep = kWaves * T::kKeys;
     const int steps = (n + kStep - 1) / kStep, per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
     const int step0 = blockIdx.y * per, step1 = min(steps, step0 + per);
     if (step0 >= step1) return;
-    auto node_at = [&](int k) { return min(max(path[k], 0), a.N - 1); };        // (used before the path has been looked over)
+    // (nodes are used before the path has been looked over; of a long path the later ones are read where they are)
+    auto node_of = [&](int node) __attribute__((always_inline)) { return min(max(node, 0), a.N - 1); };
+    if constexpr (MANY)
+        if (tid < kMaxNodes) s_path[tid] = tid <= L ? path[tid] : 0;
 
-    // query rows c kChunkRows .. into LDS
-    auto stage = [&](int c) {
-        const int r0 = c * kChunkRows, rows = min(kChunkRows, R - r0), up = (rows + 15) / 16 * 16;
-        for (int r = tid; r < up; r += kThreads) {
-            const int k = min(r0 + r, R - 1) / a.G, g = min(r0 + r, R - 1) - k * a.G, node = node_at(k);
-            const size_t at = ((size_t)b * a.N + node) * a.Hq + kvh * a.G + g;
-            s_node[r] = (int)k;
-            s_lse[r] = r < rows ? a.lse[at] * kLog2e : INFINITY;
-            s_slope[r] = a.score.slopes ? a.score.slopes[kvh * a.G + g] * kLog2e : 0.f;
+    // Query rows c kRows ..: into registers, and from there into a buffer.  A thread has 16-byte piece tid % kPieces of every kApart-th row.
+    constexpr int kPieces = T::kRowB / 16, kApart = kThreads / kPieces, kMine = T::kRows / kApart;
+    const int step_k = kApart / a.G, step_g = kApart - step_k * a.G;
+    const unsigned char* const q0 = (const unsigned char*)a.q + ((size_t)b * a.N * a.Hq + kvh * a.G) * T::kRowB + tid % kPieces * 16;
+    auto rows_of = [&](int c) __attribute__((always_inline)) { return (min(T::kRows, R - c * T::kRows) + 16 * kTogether - 1) / (16 * kTogether) * (16 * kTogether); };
+    uint4 row[kMine];
+    float row_lse = INFINITY, row_slope = 0.f;
+    int row_k = 0;
+    auto load = [&](int c, bool known) __attribute__((always_inline)) {
+        auto node_at = [&](int k) __attribute__((always_inline)) { return node_of(MANY && known && k < kMaxNodes ? s_path[k] : path[k]); };
+        const int r0 = c * T::kRows;
+        int k = (r0 + tid / kPieces) / a.G, g = r0 + tid / kPieces - k * a.G;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            row[i] = make_uint4(0, 0, 0, 0);
+            if (r0 + i * kApart < R) {                                 // (behind the last row: that one again)
+                const int kk = min(k, L), gg = k > L ? a.G - 1 : g;
+                row[i] = *(const uint4*)(q0 + ((size_t)node_at(kk) * a.Hq + gg) * T::kRowB);
+            }
+            k += step_k;
+            g += step_g;
+            if (g >= a.G) { g -= a.G; ++k; }
         }
-        for (int e = tid; e < up * (T::kRowB / 16); e += kThreads) {
-            const int r = e / (T::kRowB / 16), piece = e % (T::kRowB / 16);
-            const int rr = min(r0 + r, R - 1), k = rr / a.G, g = rr - k * a.G, node = node_at(k);
-            const uint4 v = *(const uint4*)((const unsigned char*)a.q + (((size_t)b * a.N + node) * a.Hq + kvh * a.G + g) * T::kRowB + piece * 16);
-            *(uint4*)(s_q + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = v;
+        row_lse = INFINITY;                                            // rows that do not exist give no weight
+        if (tid < T::kRows && r0 + tid < R) {
+            row_k = (r0 + tid) / a.G;
+            const int g1 = r0 + tid - row_k * a.G;
+            row_lse = a.lse[((size_t)b * a.N + node_at(row_k)) * a.Hq + kvh * a.G + g1] * kLog2e;
+            row_slope = a.score.slopes ? a.score.slopes[kvh * a.G + g1] * kLog2e : 0.f;
         }
+    };
+    auto store = [&](int buf, int c) __attribute__((always_inline)) {
+        const int piece = tid % kPieces, up = rows_of(c);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (i * kApart >= up) break;
+            const int r = tid / kPieces + i * kApart;
+            *(uint4*)(s_q[buf] + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = row[i];
+        }
+        if (tid < T::kRows) { s_lse[buf][tid] = row_lse; s_slope[buf][tid] = row_slope; s_node[buf][tid] = row_k; }
     };
 
     const int root = a.score.key_pos ? a.score.root_pos[b] : first;
@@ -115,10 +145,12 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
             const int id = a.block_table[(size_t)b * a.max_blocks + i];
             bad = bad || id < 0 || id >= a.num_pages;
         }
-    if (chunks == 1) stage(0);
+    load(0, false);
+    store(0, 0);
     bad = __syncthreads_or(bad) != 0;                                  // (every workgroup finds the same)
     if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
     if (bad) return;
+    int buf = 0;
     for (int step = step0; step < step1; ++step) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -138,47 +170,62 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
             sum[g] = 0.f;
         }
         for (int c = 0; c < chunks; ++c) {
-            if (chunks > 1) {
-                __syncthreads();
-                stage(c);
-                __syncthreads();
-            }
-            const int blocks = (min(kChunkRows, R - c * kChunkRows) + 15) / 16;
-            for (int blk = 0; blk < blocks; ++blk) {
-                f32x4 s[NG];
+            const bool more = MANY && chunks > 1 && (c + 1 < chunks || step + 1 < step1);
+            if (more) load(c + 1 < chunks ? c + 1 : 0, true);
+            const int blocks = rows_of(c) / 16;
+            for (int blk = 0; blk < blocks; blk += kTogether) {
+                f32x4 s[kTogether * NG];
 #pragma unroll
-                for (int g = 0; g < NG; ++g) s[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < kTogether * NG; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                uint4 q[kTogether][T::kT];
 #pragma unroll
-                for (int t = 0; t < T::kT; ++t) {
-                    const uint4 q = *(const uint4*)(s_q + ((blk * T::kT + t) * 64 + lane) * 16);
+                for (int u = 0; u < kTogether; ++u)
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) s[g] = product<E>(q, kf[g][t], s[g]);
+                    for (int t = 0; t < T::kT; ++t) q[u][t] = *(const uint4*)(s_q[buf] + (((blk + u) * T::kT + t) * 64 + lane) * 16);
+                f32x4 lse[kTogether], slope[kTogether];
+#pragma unroll
+                for (int u = 0; u < kTogether; ++u) {
+                    lse[u] = *(const f32x4*)(s_lse[buf] + (blk + u) * 16 + 4 * (lane >> 4));
+                    if (a.score.slopes) slope[u] = *(const f32x4*)(s_slope[buf] + (blk + u) * 16 + 4 * (lane >> 4));
                 }
-                const int r4 = blk * 16 + 4 * (lane >> 4);
-                const f32x4 lse = *(const f32x4*)(s_lse + r4), slope = *(const f32x4*)(s_slope + r4);
+#pragma unroll
+                for (int t = 0; t < T::kT; ++t)
+#pragma unroll
+                    for (int u = 0; u < kTogether; ++u)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) s[u * NG + g] = product<E>(q[u][t], kf[g][t], s[u * NG + g]);
                 if (a.score.cap_log2 > 0.f) score::cap(s, a.score);
-                float off[NG][4];                                      // to the exponent
-#pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) off[g][e] = -lse[e];
-                if (a.score.slopes) {
-#pragma unroll
-                    for (int g = 0; g < NG; ++g)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) off[g][e] = fmaf(slope[e], rel[g], -lse[e]);
-                }
                 if (own_rows) {
 #pragma unroll
-                    for (int g = 0; g < NG; ++g)
+                    for (int u = 0; u < kTogether; ++u)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (j0 + 16 * g + (lane & 15) > first + s_node[r4 + e]) s[g][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e) {
+                            const int last = first + s_node[buf][(blk + u) * 16 + 4 * (lane >> 4) + e];
+#pragma unroll
+                            for (int g = 0; g < NG; ++g)
+                                if (j0 + 16 * g + (lane & 15) > last) s[u * NG + g][e] = -INFINITY;
+                        }
                 }
+                if (a.score.slopes) {
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+                    for (int u = 0; u < kTogether; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(fmaf(s[g][e], a.score.mul, off[g][e]));
+                        for (int g = 0; g < NG; ++g)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(fmaf(s[u * NG + g][e], a.score.mul, fmaf(slope[u][e], rel[g], -lse[u][e])));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kTogether; ++u)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum[g] += fast_exp2(fmaf(s[u * NG + g][e], a.score.mul, -lse[u][e]));
+                }
+            }
+            if (more) {                                                // (what the other buffer held was read before the last barrier)
+                store(buf ^ 1, c + 1 < chunks ? c + 1 : 0);
+                __syncthreads();
+                buf ^= 1;
             }
         }
         // lane 16 g + i has key 16 g + i of the tile
@@ -197,22 +244,24 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     }
 }
 
-template <typename E, int D, int NG>
+template <typename E, int D, int NG, bool MANY>
 hipError_t launch(const WeighArgs& a, hipStream_t st) {
     const int units = a.B * a.Hkv, step = kWaves * 16 * NG, steps = (a.max_cache_len + step - 1) / step;
     int runs = (4 * a.cus + units - 1) / units;
     if (runs > steps) runs = steps;
     const dim3 grid((unsigned)units, (unsigned)runs);
-    if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false>), grid, dim3(kThreads), 0, st, a);
+    if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true, MANY>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false, MANY>), grid, dim3(kThreads), 0, st, a);
     return hipGetLastError();
 }
-// Tiles of half as many keys where whole ones would not be two workgroups for every CU.
+// Tiles of half as many keys where whole ones would not be two workgroups for every CU (32 units of 1029 keys 6.5 us and 5.8), and
+// where query rows are replaced, which takes registers.
 template <typename E, int D, int NG>
 hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
     const long long step = kWaves * 16 * NG;
-    if ((long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step) < 2 * a.cus) return launch<E, D, NG / 2>(a, st);
-    return launch<E, D, NG>(a, st);
+    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, st);
+    if ((long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step) < 2 * a.cus) return launch<E, D, NG / 2, false>(a, st);
+    return launch<E, D, NG, false>(a, st);
 }
 
 }  // namespace

@@ -13,6 +13,7 @@ namespace s4c {
 namespace {
 
 using namespace mfma;
+using parts::u32x4;                          // (arrays of HIP's uint4 are not kept in registers)
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 // 16-byte pieces of a row that a lane has: piece 4 t + lane / 16 of its row for t < T.
@@ -23,7 +24,7 @@ struct Tile {
 };
 
 template <typename E>
-__device__ __forceinline__ f32x4 product(uint4 q, uint4 k, f32x4 c) {
+__device__ __forceinline__ f32x4 product(u32x4 q, u32x4 k, f32x4 c) {
     if constexpr (sizeof(E) == 4) {
         const f32x4 x = __builtin_bit_cast(f32x4, q), y = __builtin_bit_cast(f32x4, k);
 #pragma unroll
@@ -60,59 +61,63 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     const int steps = (n + kStep - 1) / kStep, per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
     const int step0 = blockIdx.y * per, step1 = min(steps, step0 + per);
     if (step0 >= step1) return;
-    // (nodes are used before the path has been looked over; of a long path the later ones are read where they are)
+    // (nodes are used before the path has been looked over)
     auto node_of = [&](int node) __attribute__((always_inline)) { return min(max(node, 0), a.N - 1); };
     if constexpr (MANY)
         if (tid < kMaxNodes) s_path[tid] = tid <= L ? path[tid] : 0;
 
-    // Query rows c kRows ..: into registers, and from there into a buffer.  A thread has 16-byte piece tid % kPieces of every kApart-th row.
+    // Query rows c kRows ..: into registers (nothing is done with them there that would wait for them), and from there into a buffer.  A thread has 16-byte piece tid % kPieces of every kApart-th row.
     constexpr int kPieces = T::kRowB / 16, kApart = kThreads / kPieces, kMine = T::kRows / kApart;
     const int step_k = kApart / a.G, step_g = kApart - step_k * a.G;
     const unsigned char* const q0 = (const unsigned char*)a.q + ((size_t)b * a.N * a.Hq + kvh * a.G) * T::kRowB + tid % kPieces * 16;
     auto rows_of = [&](int c) __attribute__((always_inline)) { return (min(T::kRows, R - c * T::kRows) + 16 * kTogether - 1) / (16 * kTogether) * (16 * kTogether); };
-    uint4 row[kMine];
+    u32x4 row[kMine];
     float row_lse = INFINITY, row_slope = 0.f;
     int row_k = 0;
-    auto load = [&](int c, bool known) __attribute__((always_inline)) {
-        auto node_at = [&](int k) __attribute__((always_inline)) { return node_of(MANY && known && k < kMaxNodes ? s_path[k] : path[k]); };
+    auto load = [&](int c, auto in_lds) __attribute__((always_inline)) {
+        auto node_at = [&](int k) __attribute__((always_inline)) { return node_of(decltype(in_lds)::value ? s_path[k] : path[k]); };
         const int r0 = c * T::kRows;
         int k = (r0 + tid / kPieces) / a.G, g = r0 + tid / kPieces - k * a.G;
+        int node[kMine], head[kMine];
+        row_k = (r0 + tid) / a.G;
+        const int row_g = r0 + tid - row_k * a.G;
+        const bool row_on = tid < T::kRows && r0 + tid < R;
+        const int row_node = node_at(row_on ? row_k : 0);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            row[i] = make_uint4(0, 0, 0, 0);
-            if (r0 + i * kApart < R) {                                 // (behind the last row: that one again)
-                const int kk = min(k, L), gg = k > L ? a.G - 1 : g;
-                row[i] = *(const uint4*)(q0 + ((size_t)node_at(kk) * a.Hq + gg) * T::kRowB);
-            }
+        for (int i = 0; i < kMine; ++i) {                              // (behind the last row: that one again)
+            node[i] = node_at(min(k, L));
+            head[i] = k > L ? a.G - 1 : g;
             k += step_k;
             g += step_g;
             if (g >= a.G) { g -= a.G; ++k; }
         }
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            row[i] = *(const u32x4*)(q0 + ((size_t)node[i] * a.Hq + head[i]) * T::kRowB);
+        }
         row_lse = INFINITY;                                            // rows that do not exist give no weight
-        if (tid < T::kRows && r0 + tid < R) {
-            row_k = (r0 + tid) / a.G;
-            const int g1 = r0 + tid - row_k * a.G;
-            row_lse = a.lse[((size_t)b * a.N + node_at(row_k)) * a.Hq + kvh * a.G + g1] * kLog2e;
-            row_slope = a.score.slopes ? a.score.slopes[kvh * a.G + g1] * kLog2e : 0.f;
+        if (row_on) {
+            row_lse = a.lse[((size_t)b * a.N + row_node) * a.Hq + kvh * a.G + row_g];
+            if (a.score.slopes) row_slope = a.score.slopes[kvh * a.G + row_g];
         }
     };
     auto store = [&](int buf, int c) __attribute__((always_inline)) {
         const int piece = tid % kPieces, up = rows_of(c);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            if (i * kApart >= up) break;
             const int r = tid / kPieces + i * kApart;
-            *(uint4*)(s_q[buf] + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = row[i];
+            if (i * kApart < up)
+            *(u32x4*)(s_q[buf] + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = row[i];
         }
-        if (tid < T::kRows) { s_lse[buf][tid] = row_lse; s_slope[buf][tid] = row_slope; s_node[buf][tid] = row_k; }
+        if (tid < T::kRows) { s_lse[buf][tid] = row_lse * kLog2e; s_slope[buf][tid] = row_slope * kLog2e; s_node[buf][tid] = row_k; }
     };
 
     const int root = a.score.key_pos ? a.score.root_pos[b] : first;
     const size_t row0 = ((size_t)b * a.Hkv + kvh) * a.S_cap;           // of the totals and positions
-    uint4 kf[NG][T::kT], nf[NG][T::kT];
+    u32x4 kf[NG][T::kT], nf[NG][T::kT];
     int pos[NG], npos[NG];
     float total, ntotal;
-    auto fetch = [&](int step, uint4 (&f)[NG][T::kT], int (&p)[NG], float& w) __attribute__((always_inline)) {
+    auto fetch = [&](int step, u32x4 (&f)[NG][T::kT], int (&p)[NG], float& w) __attribute__((always_inline)) {
         const int j0 = __builtin_amdgcn_readfirstlane(step * kStep + wave * T::kKeys);
         size_t row = row0 + j0;
         if constexpr (PAGED) {
@@ -129,7 +134,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
             const int off = PAGED ? j - (min(j0, n - 1) & ~(T::kKeys - 1)) : j - j0;
             const unsigned char* src = (const unsigned char*)a.k_cache + (ptrdiff_t)(row + (ptrdiff_t)off) * T::kRowB + (lane >> 4) * 16;
 #pragma unroll
-            for (int t = 0; t < T::kT; ++t) f[g][t] = *(const uint4*)(src + 64 * t);
+            for (int t = 0; t < T::kT; ++t) f[g][t] = *(const u32x4*)(src + 64 * t);
             p[g] = a.score.slopes && a.score.key_pos ? a.score.key_pos[row0 + j] : j;
         }
         w = a.weight_in[row0 + min(j0 + (lane & (T::kKeys - 1)), n - 1)];
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
             const int id = a.block_table[(size_t)b * a.max_blocks + i];
             bad = bad || id < 0 || id >= a.num_pages;
         }
-    load(0, false);
+    load(0, std::false_type());
     store(0, 0);
     bad = __syncthreads_or(bad) != 0;                                  // (every workgroup finds the same)
     if (a.status && blockIdx.y == 0 && kvh == 0 && tid == 0) a.status[b] = bad ? S4C_SEQ_BAD_LEN : 0;
@@ -171,17 +176,19 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         }
         for (int c = 0; c < chunks; ++c) {
             const bool more = MANY && chunks > 1 && (c + 1 < chunks || step + 1 < step1);
-            if (more) load(c + 1 < chunks ? c + 1 : 0, true);
+            // (a choice for every row would wait for the rows before it)
+            if (more && L < kMaxNodes) load(c + 1 < chunks ? c + 1 : 0, std::true_type());
+            else if (more) load(c + 1 < chunks ? c + 1 : 0, std::false_type());
             const int blocks = rows_of(c) / 16;
             for (int blk = 0; blk < blocks; blk += kTogether) {
                 f32x4 s[kTogether * NG];
 #pragma unroll
                 for (int i = 0; i < kTogether * NG; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-                uint4 q[kTogether][T::kT];
+                u32x4 q[kTogether][T::kT];
 #pragma unroll
                 for (int u = 0; u < kTogether; ++u)
 #pragma unroll
-                    for (int t = 0; t < T::kT; ++t) q[u][t] = *(const uint4*)(s_q[buf] + (((blk + u) * T::kT + t) * 64 + lane) * 16);
+                    for (int t = 0; t < T::kT; ++t) q[u][t] = *(const u32x4*)(s_q[buf] + (((blk + u) * T::kT + t) * 64 + lane) * 16);
                 f32x4 lse[kTogether], slope[kTogether];
 #pragma unroll
                 for (int u = 0; u < kTogether; ++u) {

@@ -388,9 +388,12 @@ template <int VPR, bool PAGED>
 hipError_t launch(const EvictArgs& a, hipStream_t st) {
     const int units = a.layers * a.B * a.Hkv;
     const int keys = a.S_cap < kMostKeys ? a.S_cap : kMostKeys;
-    const bool few = a.S_cap <= 8192;
-    // Where there are units enough to fill the chip, or next to nothing to move, who selects moves as well: other units are selected meanwhile.
-    const bool whole = few && (units >= 2 * a.cus || (long long)a.list_len * a.row_bytes <= 65536);
+    // Who selects moves as well, in four waves, where there are units enough to fill the chip (others are selected meanwhile), or next to nothing to move.
+    // One launch and two, us (units x rows -> budget, bf16, head size 128): 512 x 1000 -> 700 39.7 and 41.6, 1024 x 4000 -> 2000 290 and 304, 512 x 8000 ->
+    // 4000 292 and 307, but 256 x 4000 -> 2000 88 and 82, 64 x 8000 -> 4000 127 and 56; 128 x 300 -> 200 9.6 and 17.2, but 8 x 1000 -> 700 12.2 and 10.3.
+    const bool whole = a.S_cap <= 8192 && (units >= 2 * a.cus || (a.S_cap <= 2048 && (long long)a.list_len * a.row_bytes <= 65536));
+    // (selection alone, four waves and sixteen: 128 x 2000 22.2 and 24.8, 128 x 4000 48.7 and 48.3, 128 x 8000 88.8 and 82.9 with the moving)
+    const bool few = a.S_cap <= 4096;
     hipError_t e;
     if (whole) {
         e = select<4, VPR, PAGED>(a, keys, st);

@@ -252,23 +252,24 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
 }
 
 template <typename E, int D, int NG, bool MANY>
-hipError_t launch(const WeighArgs& a, hipStream_t st) {
+hipError_t launch(const WeighArgs& a, int per_cu, hipStream_t st) {
     const int units = a.B * a.Hkv, step = kWaves * 16 * NG, steps = (a.max_cache_len + step - 1) / step;
-    int runs = (4 * a.cus + units - 1) / units;
+    int runs = (per_cu * a.cus + units - 1) / units;
     if (runs > steps) runs = steps;
     const dim3 grid((unsigned)units, (unsigned)runs);
     if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true, MANY>), grid, dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false, MANY>), grid, dim3(kThreads), 0, st, a);
     return hipGetLastError();
 }
-// Tiles of half as many keys where whole ones would not be two workgroups for every CU (32 units of 1029 keys 6.5 us and 5.8), and
-// where query rows are replaced, which takes registers.
+// Tiles of half as many keys, four workgroups for a CU (three of which run at a time), unless there are many keys: then whole tiles, two workgroups
+// for a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and 11.2; 128 x
+// 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).  Where query rows are replaced, which takes registers, half ones.
 template <typename E, int D, int NG>
 hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
-    const long long step = kWaves * 16 * NG;
-    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, st);
-    if ((long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step) < 2 * a.cus) return launch<E, D, NG / 2, false>(a, st);
-    return launch<E, D, NG, false>(a, st);
+    const long long step = kWaves * 16 * NG, steps = (long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step);
+    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, 4, st);
+    if (steps <= 16ll * a.cus) return launch<E, D, NG / 2, false>(a, 4, st);
+    return launch<E, D, NG, false>(a, 2, st);
 }
 
 }  // namespace

@@ -753,6 +753,8 @@ s4c_status s4c_verify_step(const s4c_step* p, void* hip_stream) {
 // ---- changed scores, and a cache that rows are evicted from
 namespace {
 
+constexpr int32_t kMostRows = 1 << 30;         // of a sequence: row numbers and the steps over them stay within 32 bits
+
 // (by its bits: this file is compiled without regard for NaN)
 bool is_finite(float x) {
     uint32_t u;
@@ -820,7 +822,8 @@ s4c_status weigh_impl(const s4c_attn_shape* shape, const s4c_score* score_in, co
     if (!shape_ok(shape, &why)) return why;
     if (max_path <= 0 || shape->S_cap <= 0 || max_cache_len <= 0 || max_cache_len > shape->S_cap) return S4C_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(k_cache)) return S4C_ERR_SHAPE;
-    if ((long long)shape->B * shape->Hkv > 0x7FFFFFFFll || (long long)max_path * shape->Hq > 0x3FFFFFFFll) return S4C_ERR_UNSUPPORTED;
+    if ((long long)shape->B * shape->Hkv > 0x7FFFFFFFll || (long long)max_path * shape->Hq > 0x3FFFFFFFll || shape->S_cap > kMostRows)
+        return S4C_ERR_UNSUPPORTED;
     WeighArgs a;
     if (!score_args(score_in, scale, shape->D, &a.score, &why)) return why;
     a.q = q; a.k_cache = k_cache; a.lse = lse; a.cache_len = cache_len; a.path = path; a.accept_len = accept_len;
@@ -846,7 +849,7 @@ s4c_status evict_impl(const s4c_attn_shape* shape, int32_t layers, void* k_cache
     if (!shape || !k_cache || !v_cache || !weight_in || !key_pos_in || !cache_len || !next_pos || !weight || !key_pos || !new_len)
         return S4C_ERR_NULL;
     if (!evict_sizes_ok(layers, shape->B, shape->Hkv, budget, shape->S_cap) || recent < 0 || recent > budget) return S4C_ERR_SHAPE;
-    if ((shape->D != 64 && shape->D != 128) || !dtype_ok(shape->dtype)) return S4C_ERR_UNSUPPORTED;
+    if ((shape->D != 64 && shape->D != 128) || !dtype_ok(shape->dtype) || shape->S_cap > kMostRows) return S4C_ERR_UNSUPPORTED;
     if (!aligned16(k_cache) || !aligned16(v_cache)) return S4C_ERR_SHAPE;
     const size_t need = s4c_kv_evict_workspace_size(layers, shape->B, shape->Hkv, budget, shape->S_cap);
     if (!workspace || workspace_bytes < need || (((uintptr_t)workspace) & 255)) return S4C_ERR_WORKSPACE;

@@ -66,10 +66,15 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     if constexpr (MANY)
         if (tid < kMaxNodes) s_path[tid] = tid <= L ? path[tid] : 0;
 
-    // Query rows c kRows ..: into registers (nothing is done with them there that would wait for them), and from there into a buffer.  A thread has 16-byte piece tid % kPieces of every kApart-th row.
-    constexpr int kPieces = T::kRowB / 16, kApart = kThreads / kPieces, kMine = T::kRows / kApart;
-    const int step_k = kApart / a.G, step_g = kApart - step_k * a.G;
-    const unsigned char* const q0 = (const unsigned char*)a.q + ((size_t)b * a.N * a.Hq + kvh * a.G) * T::kRowB + tid % kPieces * 16;
+    // Query rows c kRows ..: into registers (nothing is done with them there that would wait for them), and from there into a buffer.  A thread
+    // has every kThreads-th 16-byte place of the buffer, so that a wave writes a kilobyte in a row: lane r + 16 p of 64 places has piece
+    // 4 t + p of row r of a block (with a thread's pieces in one row each, 16 lanes wrote to the same banks, 1 us a chunk).
+    constexpr int kMine = T::kRows * T::kRowB / 16 / kThreads, kBlocksApart = kThreads / 64 >= T::kT ? kThreads / 64 / T::kT : 1;
+    const int my_row = ((tid >> 6) / T::kT) * 16 + (tid & 15);
+    auto my_piece = [&](int i) __attribute__((always_inline)) { return 4 * (((tid >> 6) + i * (kThreads / 64)) % T::kT) + ((tid >> 4) & 3); };
+    auto same_row = [](int i) { return (i * (kThreads / 64)) % T::kT != 0; };                 // as place i - 1
+    const int step_k = 16 * kBlocksApart / a.G, step_g = 16 * kBlocksApart - step_k * a.G;
+    const unsigned char* const q0 = (const unsigned char*)a.q + ((size_t)b * a.N * a.Hq + kvh * a.G) * T::kRowB;
     auto rows_of = [&](int c) __attribute__((always_inline)) { return (min(T::kRows, R - c * T::kRows) + 16 * kTogether - 1) / (16 * kTogether) * (16 * kTogether); };
     u32x4 row[kMine];
     float row_lse = INFINITY, row_slope = 0.f;
@@ -77,7 +82,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
     auto load = [&](int c, auto in_lds) __attribute__((always_inline)) {
         auto node_at = [&](int k) __attribute__((always_inline)) { return node_of(decltype(in_lds)::value ? s_path[k] : path[k]); };
         const int r0 = c * T::kRows;
-        int k = (r0 + tid / kPieces) / a.G, g = r0 + tid / kPieces - k * a.G;
+        int k = (r0 + my_row) / a.G, g = r0 + my_row - k * a.G;
         int node[kMine], head[kMine];
         row_k = (r0 + tid) / a.G;
         const int row_g = r0 + tid - row_k * a.G;
@@ -85,16 +90,21 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         const int row_node = node_at(row_on ? row_k : 0);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {                              // (behind the last row: that one again)
+            if (same_row(i)) {
+                node[i] = node[i - 1];
+                head[i] = head[i - 1];
+                continue;
+            }
+            if (i > 0) {
+                k += step_k;
+                g += step_g;
+                if (g >= a.G) { g -= a.G; ++k; }
+            }
             node[i] = node_at(min(k, L));
             head[i] = k > L ? a.G - 1 : g;
-            k += step_k;
-            g += step_g;
-            if (g >= a.G) { g -= a.G; ++k; }
         }
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            row[i] = *(const u32x4*)(q0 + ((size_t)node[i] * a.Hq + head[i]) * T::kRowB);
-        }
+        for (int i = 0; i < kMine; ++i) row[i] = *(const u32x4*)(q0 + ((size_t)node[i] * a.Hq + head[i]) * T::kRowB + 16 * my_piece(i));
         row_lse = INFINITY;                                            // rows that do not exist give no weight
         if (row_on) {
             row_lse = a.lse[((size_t)b * a.N + row_node) * a.Hq + kvh * a.G + row_g];
@@ -102,13 +112,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
         }
     };
     auto store = [&](int buf, int c) __attribute__((always_inline)) {
-        const int piece = tid % kPieces, up = rows_of(c);
+        const int up = rows_of(c);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int r = tid / kPieces + i * kApart;
-            if (i * kApart < up)
-            *(u32x4*)(s_q[buf] + (((r >> 4) * T::kT + (piece >> 2)) * 64 + (piece & 3) * 16 + (r & 15)) * 16) = row[i];
-        }
+        for (int i = 0; i < kMine; ++i)
+            if (((i * (kThreads / 64)) / T::kT) * 16 < up) *(u32x4*)(s_q[buf] + (tid + i * kThreads) * 16) = row[i];
         if (tid < T::kRows) { s_lse[buf][tid] = row_lse * kLog2e; s_slope[buf][tid] = row_slope * kLog2e; s_node[buf][tid] = row_k; }
     };
 

@@ -339,8 +339,8 @@ s4c_status s4c_verify_step(const s4c_step* step, void* hip_stream);
  *   s4c_tree_attn_scored -> s4c_accept_path -> s4c_kv_compact -> s4c_kv_weigh -> (root_pos += accept_len + 1) -> now and then s4c_kv_evict
  */
 typedef struct {
-    float cap;                /* > 0: a score x = scale q.k becomes cap * tanh(x / cap); 0: it stays.  2 cap log2(e) and scale / cap
-                                 must be finite in fp32 */
+    float cap;                /* > 0: a score x = scale q.k becomes cap * tanh(x / cap); 0: it stays.  cap and scale / cap lie
+                                 between 2^-90 and 2^90 */
     const float* slopes;      /* [Hq] nullable: slopes[h] * (position of the key - position of the root) is added to it (a penalty on
                                  distance has slopes > 0).  For a node of depth d this differs from the distance to the node by
                                  slopes[h] * d on every key, which changes lse and not the output */
@@ -353,8 +353,8 @@ typedef struct {
 /* s4c_tree_attn with changed scores.  Everything not named here is as in s4c_tree_attn (workspace size, status, limits).
  *   score  host pointer, nullable (nothing changed)
  *   lse    [B][N][Hq] fp32 nullable: natural log of the sum of exp(changed score) over the keys that the row sees; +infinity for
- *          the rows of a flagged sequence.  The biggest error is that of the scores, which are fp32.
- * Results are deterministic; with no cap and no slopes `out` is s4c_tree_attn's up to rounding of the scores. */
+ *          the rows of a flagged sequence.
+ * Scores and statistics are fp32 (a cap's tanh is off by less than 2^-22 of itself).  Results are deterministic. */
 s4c_status s4c_tree_attn_scored(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree,
                                 const void* v_tree, const void* k_cache, const void* v_cache, const int32_t* cache_len,
                                 const int32_t* parent, int32_t max_cache_len, float scale, void* out, float* lse, int32_t* status,
@@ -377,7 +377,7 @@ s4c_status s4c_tree_attn_scored_paged(const s4c_attn_shape* shape, const s4c_sco
  *              root_pos + k); root_pos is the root's of that attention call
  *   weight_in, weight  [B][Hkv][S_cap] fp32, the same array or two that do not overlap; rows from cache_len[b] on are not written
  *   status     [B] nullable: S4C_SEQ_BAD_LEN if cache_len, accept_len, the path or a page is not valid; nothing of that sequence is written.
- * Sums are fp32 in a fixed order: results are deterministic. */
+ * S_cap <= 2^30.  Sums are fp32 in a fixed order: results are deterministic. */
 s4c_status s4c_kv_weigh(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_cache, const float* lse,
                         const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path,
                         int32_t max_cache_len, float scale, const float* weight_in, float* weight, int32_t* status, void* hip_stream);
@@ -397,8 +397,9 @@ s4c_status s4c_kv_weigh_paged(const s4c_attn_shape* shape, const s4c_score* scor
  *   new_len  [B] the length after, min(cache_len, budget) (may be cache_len itself)
  *   kept     [layers][B][Hkv][budget] nullable: the row that row i was before, -1 behind the new length
  *   status   [B] nullable: S4C_SEQ_BAD_LEN if cache_len or a page is not valid; then only new_len (unchanged) and kept (-1) are written.
- *   workspace >= s4c_kv_evict_workspace_size(...) bytes, 256-byte aligned, contents need not be initialised
- * Only B, Hkv, D, S_cap and dtype of `shape` are used.  Cache rows from the new length on are left as they were. */
+ *   workspace >= s4c_kv_evict_workspace_size(...) bytes, 256-byte aligned, contents need not be initialised; two calls that may overlap
+ *            in time (captured graphs among them) must not share it
+ * Only B, Hkv, D, S_cap (<= 2^30) and dtype of `shape` are used.  Cache rows from the new length on are left as they were. */
 size_t s4c_kv_evict_workspace_size(int32_t layers, int32_t B, int32_t Hkv, int32_t budget, int32_t S_cap);
 s4c_status s4c_kv_evict(const s4c_attn_shape* shape, int32_t layers, void* k_cache, void* v_cache, const float* weight_in,
                         const int32_t* key_pos_in, const int32_t* cache_len, const int32_t* next_pos, int32_t budget, int32_t recent,

@@ -769,11 +769,12 @@ bool score_args(const s4c_score* sc, float scale, int32_t D, score::Changed* a, 
     a->slope_mul = kLog2e / a->mul;
     if (!sc) return true;
     if (sc->key_pos && !sc->root_pos) { *why = S4C_ERR_NULL; return false; }
+    constexpr float kLeast = 0x1p-90f, kMost = 0x1p90f;         // (products with what is capped stay in fp32's normal numbers)
     if (!is_finite(sc->cap) || sc->cap < 0.f) { *why = S4C_ERR_SHAPE; return false; }
     if (sc->cap > 0.f) {
         a->cap_log2 = sc->cap * kLog2e;
         a->to_y = scale / sc->cap;
-        if (!is_finite(2.f * a->cap_log2) || !is_finite(a->to_y)) { *why = S4C_ERR_SHAPE; return false; }
+        if (sc->cap < kLeast || sc->cap > kMost || !is_finite(a->to_y) || a->to_y < kLeast || a->to_y > kMost) { *why = S4C_ERR_SHAPE; return false; }
         a->mul = 1.f;
         a->slope_mul = kLog2e;
         // (where a coefficient leaves fp32's normal numbers, the fit that takes y does)
@@ -785,6 +786,7 @@ bool score_args(const s4c_score* sc, float scale, int32_t D, score::Changed* a, 
             a->fit[i] = (float)(kFour[i] * c);
             normal = normal && fabs(kFour[i] * c) > 1e-37 && fabs(kFour[i] * c) < 1e37;
         }
+        for (int i = 0; i < 4 && !normal; ++i) a->fit[i] = 0.f;       // (still asked for where all products are 0)
         a->fit_up_to = normal ? 0.35f / a->to_y : 0.f;
     }
     a->slopes = sc->slopes;

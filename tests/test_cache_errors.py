@@ -28,7 +28,7 @@ def test_scored_attention():
     assert at(q=None) == -1 and at(sh=shape(N=129)) == -3 and at(sh=shape(Hq=7)) == -2 and at(m=1 << 20) == -2
     assert at(q=C.c_void_p(264)) == -2
     assert B.s4c_tree_attn_workspace_size(shape(), 4096) > 0 and at(ws=None) == -4 and at(wsb=8) == -4
-    for cap in (-1.0, float("nan"), float("inf"), -float("inf"), 3.3e38, 1e-40):
+    for cap in (-1.0, float("nan"), float("inf"), -float("inf"), 3.3e38, 1e-40, 1e28, 1e-28):
         assert at(sc=score(cap)) == -2, cap
     assert at(sc=score(0.0, ONE, ONE, None)) == -1
     pg = lambda sh=shape(), bt=ONE, mb=64, ps=128, npg=200, pool=ONE: L.s4c_tree_attn_scored_paged(
@@ -44,7 +44,7 @@ def test_weights():
         assert w(**kw) == -1, kw
     assert w(sh=shape(D=96)) == -3 and w(sh=shape(N=200)) == -3 and w(sh=shape(dtype=9)) == -3
     assert w(mp=0) == -2 and w(m=0) == -2 and w(m=1 << 20) == -2 and w(k=C.c_void_p(8)) == -2 and w(sc=score(-1.0)) == -2
-    assert w(mp=1 << 28) == -3
+    assert w(mp=1 << 28) == -3 and w(sh=shape(S_cap=(1 << 30) + 1)) == -3
     pg = lambda bt=ONE, mb=64, ps=128, npg=200: L.s4c_kv_weigh_paged(C.byref(shape()), score(), ONE, ONE, bt, mb, ps, npg, ONE, ONE, ONE, ONE, 4,
                                                                      4096, 0.0, ONE, ONE, None, None)
     assert pg(bt=None) == -1 and pg(ps=32) == -3 and pg(mb=0) == -2 and pg(mb=65) == -2 and pg(npg=-1) == -2
@@ -64,7 +64,7 @@ def test_eviction():
     for kw in (dict(layers=0), dict(layers=70000), dict(budget=0), dict(recent=-1), dict(recent=101), dict(k=C.c_void_p(24)), dict(sh=shape(B=0)),
                dict(sh=shape(S_cap=0))):
         assert ev(**kw) == -2, kw
-    assert ev(sh=shape(D=80)) == -3 and ev(sh=shape(dtype=5)) == -3
+    assert ev(sh=shape(D=80)) == -3 and ev(sh=shape(dtype=5)) == -3 and ev(sh=shape(S_cap=(1 << 30) + 1)) == -3
     assert ev(ws=None) == -4 and ev(wsb=size(1, 2, 2, 100, 8192) - 1) == -4 and ev(ws=C.c_void_p(128)) == -4
     pg = lambda bt=ONE, mb=64, ps=128, npg=200: L.s4c_kv_evict_paged(C.byref(shape()), 1, ONE, ONE, bt, mb, ps, npg, ONE, ONE, ONE, ONE, 100, 10,
                                                                      ONE, ONE, ONE, None, None, ONE, 1 << 20, None)

@@ -118,6 +118,25 @@ def test_weights_against_the_definition(name, dtype):
         assert torch.equal(c.win[b, :, :n], c.w[b, :, :n]) and torch.equal(c.win[b, :, n:], before[b, :, n:])
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_weights_of_random_shapes(seed):
+    r = np.random.default_rng([seed, 6])
+    D, G, Hkv, B_ = int(r.choice([64, 128])), int(r.choice([1, 2, 3, 5, 8])), int(r.choice([1, 2, 3])), int(r.integers(1, 4))
+    N = int(r.choice([1, 2, r.integers(3, 129)]))
+    page = int(r.choice([0, 0, 64, 128]))
+    acc = [int(r.integers(0, N)) for _ in range(B_)]
+    S_cap = -(-max(int(np.exp(r.uniform(np.log(4), np.log(1500)))), N) // (page or 8)) * (page or 8)
+    lengths = [int(r.integers(a + 1, S_cap + 1)) for a in acc]
+    c = Weigh(seed + 200, B_, N, Hkv * G, Hkv, D, str(r.choice(["bf16", "f16", "f32"])), lengths, acc, S_cap, page, max_path=N)
+    for _ in range(2):
+        s = c.score(float(r.choice([0.0, 1.0, 10.0, 40.0])), str(r.choice(["none", "rows", "kept"])))
+        want = c.want(s)
+        before = c.w.fill_(7.0).clone()
+        c.call(s, m=int(r.integers(max(lengths), S_cap + 1)))
+        assert not c.status.any()
+        c.check(s, want, c.w, before)
+
+
 def test_weights_with_a_node_named_twice_and_a_scale():
     """The path is what it says, whatever nodes it names; `scale` is the caller's."""
     c = Weigh(3, 2, 7, 4, 2, 64, "bf16", (90, 77), (3, 3), 96, node=[0, 5, 5, 2])
@@ -314,6 +333,41 @@ def test_eviction_of_long_units():
     for n, budget in ((32768, 20000), (32769, 32000), (70001, 30011)):
         c = Evict(n, 1, 2, 1, 64, "bf16", (n, n - 9000), n, 0, "ties")
         c.check(budget, 999)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_eviction_of_random_shapes(seed):
+    r = np.random.default_rng([seed, 7])
+    layers, B_, Hkv, D = int(r.choice([1, 1, 3])), int(r.integers(1, 4)), int(r.choice([1, 2, 5])), int(r.choice([64, 128]))
+    page = int(r.choice([0, 0, 64, 256]))
+    S_cap = -(-int(np.exp(r.uniform(np.log(3), np.log(10000 // (layers * Hkv))))) // (page or 1)) * (page or 1)
+    c = Evict(seed + 300, layers, B_, Hkv, D, str(r.choice(["bf16", "f16", "f32"])), [int(r.integers(0, S_cap + 1)) for _ in range(B_)], S_cap, page,
+              str(r.choice(["spread", "ties", "signed"])))
+    budget = int(r.integers(1, S_cap + 2))
+    c.check(budget, int(r.integers(0, budget + 1)), in_place=bool(r.random() < 0.5))
+
+
+def test_more_recent_rows_than_the_budget():
+    """Positions that are all recent (nothing says that they differ): the first rows stay."""
+    c = Evict(8, 1, 2, 2, 64, "bf16", (300, 77), 320)
+    c.pos.fill_(int(c.next[0]) - 1)
+    c.check(50, 10)
+    assert c.kept[0, 0, 0].tolist() == list(range(50))
+
+
+def test_totals_that_are_not_numbers_stay_in_bounds():
+    """Which rows stay is open, but they are rows of the sequence, each once, and every row is where kept says."""
+    c = Evict(9, 1, 2, 2, 64, "bf16", (200, 150), 256)
+    c.w[0, 0].fill_(float("nan"))
+    c.w[0, 1, :, ::3] = float("nan")
+    c.w[0, 1, 1, 1::3] = -float("nan")
+    old = c.kc.clone()
+    c.run(100, 20)
+    for b, n in ((0, 200), (1, 150)):
+        for h in range(2):
+            k = c.kept[0, b, h].long()
+            assert int(k.min()) >= 0 and int(k.max()) < n and len(set(k.tolist())) == 100
+            assert torch.equal(c.kc[0, b, h, :100], old[0, b, h, k])
 
 
 def test_evicted_twice():

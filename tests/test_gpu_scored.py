@@ -140,6 +140,41 @@ def test_scores_far_beyond_the_cap(dtype):
         c.check(c.score(cap, "none"))
 
 
+@pytest.mark.parametrize("N", [7, 80])
+def test_caps_at_the_ends_of_their_range(N):
+    """A cap so wide that it does nothing, one so narrow that only signs are left, and scores that are all zero."""
+    c = Case(14, 1, N, 4, 2, 128, "bf16", (200,), 256)
+    for cap in (1e20, 1e5, 1e-3, 1e-20):
+        c.call(c.score(cap, "rows"))
+        c.check(c.score(cap, "rows"))
+        c.call(c.score(cap, "none"))
+        c.check(c.score(cap, "none"))
+    c.q.zero_()
+    for cap in (1e20, 30.0, 1e-20):
+        c.call(c.score(cap, "none"))
+        c.check(c.score(cap, "none"))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes(seed):
+    r = np.random.default_rng([seed, 5])
+    D, G, Hkv, B_ = int(r.choice([64, 128])), int(r.choice([1, 2, 3, 4, 8])), int(r.choice([1, 2, 3])), int(r.integers(1, 4))
+    N = int(r.choice([1, 2, r.integers(3, 129)]))
+    page = int(r.choice([0, 0, 64, 128]))
+    top = int(np.exp(r.uniform(np.log(4), np.log(1200))))
+    while N * G * Hkv * B_ * top > 400000:
+        top //= 2
+    lengths = [int(r.integers(0, top + 1)) for _ in range(B_)]
+    S_cap = -(-max(top, 1) // (page or 8)) * (page or 8)
+    c = Case(seed + 100, B_, N, Hkv * G, Hkv, D, str(r.choice(["bf16", "f16", "f32"])), lengths, S_cap, page, chain=bool(r.random() < 0.3))
+    for _ in range(2):
+        s = c.score(float(r.choice([0.0, 1.0, 10.0, 40.0])), str(r.choice(["none", "rows", "kept"])))
+        c.out.fill_(7.0)
+        c.lse.fill_(7.0)
+        c.call(s, max_len=int(r.integers(max(lengths), S_cap + 1)))
+        c.check(s)
+
+
 def test_another_scale_and_a_longer_bound():
     """`scale` is the caller's; max_cache_len only sizes the launch."""
     c = Case(6, 2, 10, 4, 2, 128, "f16", (90, 300), 1024)

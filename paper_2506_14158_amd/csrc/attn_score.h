@@ -6,9 +6,10 @@
 // keys of a row, and the softmax does not see it.  Positions are differences of 32-bit integers first and fp32 after: exact up to 2^24.
 //
 // What it costs is operations of the vector ALUs, of which a score otherwise has about eight (four of them its exponential):
-//   bias by rows      one: the tile's own distance goes to the reference that the exponentials are taken against, a key's distance inside the
-//                     tile is a constant; the bias is added to the bare product (slopes are divided by the scale once)
-//   bias looked up    three: difference, conversion, addition
+//   bias              for many rows none: an fp32 product of the keys' distances and the rows' slopes is added by the matrix cores, 64 cycles for 32 x 32
+//                     scores (slopes are divided by the scale once, so that it goes to the bare products).  For few rows, where a wave waits for that, one
+//                     by rows (the tile's own distance goes to the reference of the exponentials), three where positions are looked up.  The one and the
+//                     other, us: 16 x 64/8 heads, 32768 keys + 128 nodes, looked up 2105 and 2200; 13 x 32/8 heads, 5003 keys, one node 28.6 and 25.1
 //   cap               C y p(y^2), y = x / cap, C = cap log2(e), p a fit of tanh(y)/y at Chebyshev nodes.  Where all scores of a wave are within 0.35
 //                     of the cap (and nothing is added), the kernel for many rows takes four terms (relative error 3.5e-8) with the scale in the
 //                     coefficients, and the last product is the one that makes the exponent: four more operations.  Within 0.6 five terms (7.5e-8).  Beyond, C - 2 C / (1 +
@@ -97,41 +98,36 @@ struct Factor<false> {
     __device__ __forceinline__ float operator()(float) const { return mul; }
 };
 
-// Register j of a lane is key 8 (j/4) + j%4 of the lane's part of a block of 32; a tile has BLOCKS of them.
+// The bias of a block of 32 keys and 32 rows is the product of a column and a row, which the matrix cores add: `distance` is the position of key
+// lane % 32 from the root's, `slope` that of row lane % 32 (the instruction's second term is 0).
+__device__ __forceinline__ f32x16 add_bias(float distance, float slope, const f32x16& s) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32((threadIdx.x & 32) == 0 ? distance : 0.f, slope, s, 0, 0, 0);
+}
+// The same by the vector ALUs.  Register j of a lane is key 8 (j/4) + j%4 of the lane's part of a block.
 // ... whose first key is row `first` before (< 0) or behind the root; returns what is left to add to the lane's scores, in log2 units.
 // (Counted from the part's last key, the one next to the root: there the sums are small, and so are their roundings.)
-template <int BLOCKS>
-__device__ __forceinline__ float add_rows(f32x16 (&s)[BLOCKS], float slope, int first, const Changed& a) {
-    constexpr int kLast = 32 * BLOCKS - 5;
+__device__ __forceinline__ float add_rows(f32x16& s, float slope, int first, const Changed& a) {
 #pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[k][j] = fmaf((float)(32 * k + 8 * (j >> 2) + (j & 3) - kLast), slope, s[k][j]);
-    return slope * a.mul * (float)(first + kLast);
+    for (int j = 0; j < 16; ++j) s[j] = fmaf((float)(8 * (j >> 2) + (j & 3) - 27), slope, s[j]);
+    return slope * a.mul * (float)(first + 27);
 }
 // ... whose positions lie in LDS
-template <int BLOCKS>
-__device__ __forceinline__ void add_looked_up(f32x16 (&s)[BLOCKS], float slope, const int32_t* pos, int root) {
+__device__ __forceinline__ void add_looked_up(f32x16& s, float slope, const int32_t* pos, int root) {
 #pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
+    for (int q = 0; q < 4; ++q) {
+        const i32x4 p = *(const i32x4*)(pos + 8 * q);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const i32x4 p = *(const i32x4*)(pos + 32 * k + 8 * q);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[k][4 * q + e] = fmaf(slope, (float)(p[e] - root), s[k][4 * q + e]);
-        }
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, (float)(p[e] - root), s[4 * q + e]);
+    }
 }
 // ... of nodes of the tree
-template <int BLOCKS>
-__device__ __forceinline__ void add_depths(f32x16 (&s)[BLOCKS], float slope, const float* depth) {
+__device__ __forceinline__ void add_depths(f32x16& s, float slope, const float* depth) {
 #pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
+    for (int q = 0; q < 4; ++q) {
+        const f32x4 d = *(const f32x4*)(depth + 8 * q);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 d = *(const f32x4*)(depth + 32 * k + 8 * q);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[k][4 * q + e] = fmaf(slope, d[e], s[k][4 * q + e]);
-        }
+        for (int e = 0; e < 4; ++e) s[4 * q + e] = fmaf(slope, d[e], s[4 * q + e]);
+    }
 }
 // every node's depth, by the thread that has written its ancestors
 __device__ __forceinline__ void note_depth(const AttnArgs& a, const uint32_t* anc, float* depth) {

@@ -46,6 +46,8 @@ template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, 
 __global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
     constexpr bool kScored = SCORE != score::kPlain;
+    // Slopes make the largest score of a row grow from tile to tile, and bf16 has room for exponentials that are far above 1.
+    constexpr float kLag = !F16 && (SCORE == score::kSlopes || SCORE == score::kCapSlopes) ? 64.0f : kLazyLog2;
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row
@@ -330,6 +332,15 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         constexpr int MODE = decltype(mode_tag)::value;
         const lds_u8* stage = (const lds_u8*)smem + ((uint32_t)done % NS) * kStageB;     // LDS address space throughout
 
+        // key lane % 32 of a block, from the root (changed scores)
+        auto distance = [&](int kblk) __attribute__((always_inline)) {
+            const int in = 32 * kblk + (lane & 31);
+            if constexpr (MODE == kTree) return depths[arg * kBN + in];
+            else if constexpr (kScored) {
+                const int p = ring_pos[((uint32_t)done % NS) * kBN + in];
+                return (float)(sc.key_pos ? p - root : key0 + in - P);
+            } else return 0.f;
+        };
         // S^T = K Q^T for the two 32-key blocks.  The two accumulator chains are interleaved (a
         // dependent MFMA cannot start before its predecessor retires); the K fragments of the
         // second half of the head dimension are requested while the first half is multiplied.
@@ -343,6 +354,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) { s[0][j] = 0.f; s[1][j] = 0.f; }
+            if constexpr (SCORE == score::kSlopes) {
+                s[0] = score::add_bias(distance(0), slope, s[0]);
+                s[1] = score::add_bias(distance(1), slope, s[1]);
+            }
             if constexpr (kKT == 8) {
 #pragma unroll
                 for (int tt = 0; tt < 4; ++tt) {
@@ -369,16 +384,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         }
 
         // ---- changed scores
-        float mul = a.scale_log2, off = 0.f;                  // to log2 units
+        float mul = a.scale_log2;                             // to log2 units
         bool fits = false;
         if constexpr (kScored) {
             mul = sc.mul;
-            auto add_positions = [&]() __attribute__((always_inline)) {
-                if constexpr (MODE == kTree) score::add_depths(s, slope, depths + arg * kBN + 4 * g32);
-                else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + ((uint32_t)done % NS) * kBN + 4 * g32, root);
-                else off = score::add_rows(s, slope, key0 + 4 * g32 - P, sc);
-            };
-            if constexpr (SCORE == score::kSlopes) add_positions();
             if constexpr (SCORE == score::kCap || SCORE == score::kCapSlopes) {
                 if constexpr (MODE == kPlain) {
                     float most = fmaxf(fabsf(s[0][0]), fabsf(s[1][0]));
@@ -399,7 +408,8 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
 #pragma unroll
                         for (int j = 0; j < 16; ++j) s[kblk][j] *= capped(s[kblk][j]);
                 }
-                add_positions();
+                s[0] = score::add_bias(distance(0), slope, s[0]);
+                s[1] = score::add_bias(distance(1), slope, s[1]);
             }
         }
         const score::Factor<SCORE == score::kCap && MODE == kPlain> factor(sc, fits, mul);
@@ -426,7 +436,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int j = 1; j < 16; ++j) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[0][j]), s[1][j]);    // v_max3_f32
-        if constexpr (kScored) mx = fmaf(mx, factor(mx), off);        // (tanh grows with its argument; the halves have different keys: before they meet)
+        if constexpr (kScored) mx *= factor(mx);                      // (tanh grows with its argument)
         mx = max_across_halves(mx);
         float psum = 0.f;
         if constexpr (MODE == kPlain) {
@@ -437,7 +447,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             // consistent with whatever reference is current, which is all the final division (or the
             // merge of KV splits) needs.
             const float mt = kScored ? mx : mx * mul;
-            if (__any(mt > m_run + kLazyLog2)) {
+            if (__any(mt > m_run + kLag)) {
                 const float m_new = fmaxf(m_run, mt);
                 const float alpha = fast_exp2(m_run - m_new);          // first tile: exp2(-inf) = 0
                 l_run *= alpha;
@@ -451,7 +461,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], factor(s[kblk][j]), kScored ? off + (kShift - m_run) : kShift - m_run));
+                    const float p = fast_exp2(fmaf(s[kblk][j], factor(s[kblk][j]), kShift - m_run));
                     s[kblk][j] = p;
                     psum += p;
                 }
@@ -465,7 +475,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             for (int kblk = 0; kblk < 2; ++kblk)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float p = fast_exp2(fmaf(s[kblk][j], mul, kScored ? off + (kShift - m_safe) : kShift - m_safe));
+                    const float p = fast_exp2(fmaf(s[kblk][j], mul, kShift - m_safe));
                     s[kblk][j] = p;
                     psum += p;
                 }

@@ -406,10 +406,9 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
                 mul = sc.mul;
                 if (sc.cap_log2 > 0.f) score::cap(s, sc);
                 if (sc.slopes) {
-                    f32x16(&one)[1] = reinterpret_cast<f32x16(&)[1]>(s);
-                    if (MASKED && my >= u_pref) score::add_depths(one, slope, depths + (my - u_pref) * kBN + 4 * g32);
-                    else if (sc.key_pos) score::add_looked_up(one, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);
-                    else off = score::add_rows(one, slope, my * kBN + 4 * g32 - P, sc);
+                    if (MASKED && my >= u_pref) score::add_depths(s, slope, depths + (my - u_pref) * kBN + 4 * g32);
+                    else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);
+                    else off = score::add_rows(s, slope, my * kBN + 4 * g32 - P, sc);
                 }
             }
             if constexpr (MASKED) {

@@ -343,7 +343,8 @@ typedef struct {
                                  between 2^-90 and 2^90 */
     const float* slopes;      /* [Hq] nullable: slopes[h] * (position of the key - position of the root) is added to it (a penalty on
                                  distance has slopes > 0).  For a node of depth d this differs from the distance to the node by
-                                 slopes[h] * d on every key, which changes lse and not the output */
+                                 slopes[h] * d on every key, which changes lse and not the output.  Without a cap, scale lies between
+                                 2^-60 and 2^60 then */
     int32_t* key_pos;         /* [B][Hkv][S_cap] nullable: position of every cache row.  NULL: row j has position j, and the root
                                  the position of the row that it is appended to.  Read only where slopes are given; s4c_kv_weigh
                                  writes those of the path's rows */
@@ -406,7 +407,8 @@ s4c_status s4c_kv_evict(const s4c_attn_shape* shape, int32_t layers, void* k_cac
                         float* weight, int32_t* key_pos, int32_t* new_len, int32_t* kept, int32_t* status, void* workspace,
                         size_t workspace_bytes, void* hip_stream);
 /* ... of paged pools [layers][num_pages][Hkv][page_size][D] behind one block table (as in s4c_commit_path_paged): shape->S_cap =
- * max_blocks * page_size, totals and positions by logical row.  Pages that hold no row below the new length are free afterwards. */
+ * max_blocks * page_size, totals and positions by logical row.  Rows below the lengths are written, so no two sequences may share a page.
+ * Pages that hold no row below the new length are free afterwards. */
 s4c_status s4c_kv_evict_paged(const s4c_attn_shape* shape, int32_t layers, void* k_pool, void* v_pool, const int32_t* block_table,
                               int32_t max_blocks, int32_t page_size, int32_t num_pages, const float* weight_in,
                               const int32_t* key_pos_in, const int32_t* cache_len, const int32_t* next_pos, int32_t budget,

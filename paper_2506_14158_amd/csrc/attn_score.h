@@ -12,8 +12,9 @@
 //                     other, us: 16 x 64/8 heads, 32768 keys + 128 nodes, looked up 2105 and 2200; 13 x 32/8 heads, 5003 keys, one node 28.6 and 25.1
 //   cap               C y p(y^2), y = x / cap, C = cap log2(e), p a fit of tanh(y)/y at Chebyshev nodes.  Where all scores of a wave are within 0.35
 //                     of the cap (and nothing is added), the kernel for many rows takes four terms (relative error 3.5e-8) with the scale in the
-//                     coefficients, and the last product is the one that makes the exponent: four more operations.  Within 0.6 five terms (7.5e-8).  Beyond, C - 2 C / (1 +
-//                     exp2(2 log2(e) y)), two more operations at a quarter of the rate, off by C 2^-23, a relative 2.2e-7 there.
+//                     coefficients, and the last product is the one that makes the exponent: four more operations.  Within 0.6 five
+//                     terms (7.5e-8).  Beyond, C - 2 C / (1 + exp2(2 log2(e) y)), two more operations at a quarter of the rate, off by C 2^-23,
+//                     a relative 2.2e-7 there.
 #pragma once
 #include "common.h"
 
@@ -43,9 +44,9 @@ __device__ __forceinline__ float beyond(float y, float c) {
     return fmaf(-2.f * c, __builtin_amdgcn_rcpf(1.f + e), c);
 }
 
-// products -> capped scores in log2 units (cap > 0); N values, s(j) a reference to the j-th
+// products -> c tanh(to_y product) (cap > 0); N values, s(j) a reference to the j-th
 template <int N, class V>
-__device__ __forceinline__ void cap_all(V s, const Changed& a) {
+__device__ __forceinline__ void cap_all(V s, const Changed& a, float c) {
     float most = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -54,37 +55,38 @@ __device__ __forceinline__ void cap_all(V s, const Changed& a) {
     }
     if (!__any(most > kFitUpTo)) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) s(j) = fitted(s(j), a.cap_log2);
+        for (int j = 0; j < N; ++j) s(j) = fitted(s(j), c);
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) s(j) = fabsf(s(j)) <= kFitUpTo ? fitted(s(j), a.cap_log2) : beyond(s(j), a.cap_log2);
+        for (int j = 0; j < N; ++j) s(j) = fabsf(s(j)) <= kFitUpTo ? fitted(s(j), c) : beyond(s(j), c);
     }
 }
 // ... of a tile of 32 keys (a lane's register j), and of NG blocks of 16 x 16
-__device__ __forceinline__ void cap(f32x16& s, const Changed& a) {
+__device__ __forceinline__ void cap(f32x16& s, const Changed& a, float c) {
     float x[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = s[j];
-    cap_all<16>([&](int j) -> float& { return x[j]; }, a);
+    cap_all<16>([&](int j) -> float& { return x[j]; }, a, c);
 #pragma unroll
     for (int j = 0; j < 16; ++j) s[j] = x[j];
 }
 template <int NG>
-__device__ __forceinline__ void cap(f32x4 (&s)[NG], const Changed& a) {
+__device__ __forceinline__ void cap(f32x4 (&s)[NG], const Changed& a, float c) {
     float x[4 * NG];
 #pragma unroll
     for (int j = 0; j < 4 * NG; ++j) x[j] = s[j >> 2][j & 3];
-    cap_all<4 * NG>([&](int j) -> float& { return x[j]; }, a);
+    cap_all<4 * NG>([&](int j) -> float& { return x[j]; }, a, c);
 #pragma unroll
     for (int j = 0; j < 4 * NG; ++j) s[j >> 2][j & 3] = x[j];
 }
 // What a value of a tile is multiplied with to be a score in log2 units.  FIT: a product within fit_up_to is capped by it, s p(s^2) in
-// all; one that has been capped otherwise is multiplied by 1 with the same instructions, so that one line of code lies behind the choice.
+// all; one that is a tanh already is multiplied by the cap with the same instructions, so that one line of code lies behind the choice (a tanh, and
+// not what it is multiplied to: that one's square can be infinite).
 template <bool FIT>
 struct Factor {
     float c[4];
     __device__ __forceinline__ Factor(const Changed& a, bool fits, float)
-        : c{fits ? a.fit[0] : 1.f, fits ? a.fit[1] : 0.f, fits ? a.fit[2] : 0.f, fits ? a.fit[3] : 0.f} {}
+        : c{fits ? a.fit[0] : a.cap_log2, fits ? a.fit[1] : 0.f, fits ? a.fit[2] : 0.f, fits ? a.fit[3] : 0.f} {}
     __device__ __forceinline__ float operator()(float s) const {
         const float z = s * s;
         return fmaf(z, fmaf(z, fmaf(z, c[3], c[2]), c[1]), c[0]);

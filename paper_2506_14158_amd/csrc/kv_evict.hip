@@ -9,8 +9,9 @@
 // are kept in LDS (longer units are read again for every sweep).  The smallest key that stays is found by a radix descent, 11, 11
 // and 10 bits from the top: a histogram in LDS, which every wave scans by itself (a barrier less, and nothing to hand over), and the last digits are
 // left out where all rows of a bin stay, as they do as soon as totals differ.  Places and movers are listed in row order by ballots.  What bounds it is
-// the instructions of one CU on a long unit (32768 rows: 52 us before keys were looked at as few times and with as few instructions as they are now).
-// Moving is a copy, bound by memory.
+// the instructions of one CU on a long unit: 128 units of up to 32768 rows 28 us (keys read from memory in every sweep 94, more instructions a key 54).
+// Moving is a copy, bound by memory: 9500 rows of 256 bytes of each of them, K and V, 167 us (833 MB, 5.0 TB/s).
+// 32 layers of 32 heads, 1367 -> 1024 rows, in one launch 79 us, 355 MB at 4.5 TB/s.
 #include "mfma_common.h"
 
 namespace s4c {

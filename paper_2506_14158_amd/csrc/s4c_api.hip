@@ -789,6 +789,8 @@ bool score_args(const s4c_score* sc, float scale, int32_t D, score::Changed* a, 
         for (int i = 0; i < 4 && !normal; ++i) a->fit[i] = 0.f;       // (still asked for where all products are 0)
         a->fit_up_to = normal ? 0.35f / a->to_y : 0.f;
     }
+    // (slopes are divided by what comes after them: a quotient times any distance stays finite)
+    if (sc->slopes && !(sc->cap > 0.f) && (scale < 0x1p-60f || scale > 0x1p60f)) { *why = S4C_ERR_SHAPE; return false; }
     a->slopes = sc->slopes;
     a->key_pos = sc->key_pos;
     a->root_pos = sc->root_pos;

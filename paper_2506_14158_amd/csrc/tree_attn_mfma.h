@@ -396,8 +396,9 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
                     fits = !__any(most > sc.fit_up_to);
                 }
                 if (MODE != kPlain || __builtin_expect(!fits, 0)) {
-                    score::cap(s[0], sc);
-                    score::cap(s[1], sc);
+                    const float c = MODE == kPlain ? 1.f : sc.cap_log2;
+                    score::cap(s[0], sc, c);
+                    score::cap(s[1], sc, c);
                 }
             }
             if constexpr (SCORE == score::kCapSlopes) {

@@ -404,7 +404,7 @@ void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE>
             float mul = a.scale_log2, off = 0.f;              // to log2 units
             if constexpr (kScored) {
                 mul = sc.mul;
-                if (sc.cap_log2 > 0.f) score::cap(s, sc);
+                if (sc.cap_log2 > 0.f) score::cap(s, sc, sc.cap_log2);
                 if (sc.slopes) {
                     if (MASKED && my >= u_pref) score::add_depths(s, slope, depths + (my - u_pref) * kBN + 4 * g32);
                     else if (sc.key_pos) score::add_looked_up(s, slope, ring_pos + (((uint32_t)done % kNR) * kKG + kg) * kBN + 4 * g32, root);

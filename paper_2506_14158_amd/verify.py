@@ -66,6 +66,8 @@ class TreeVerifier:
 
     def kv_evict(self, k_cache, v_cache, weight, key_pos, cache_len, next_pos):
         """Every layer's cache [layers][B][Hkv][S_cap][D] down to self.budget rows, with its totals and positions, all in place."""
+        if self.budget <= 0:
+            raise ValueError("a verifier without a budget evicts nothing")
         _b.s4c_kv_evict(k_cache, v_cache, weight, key_pos, cache_len, next_pos, self.budget, self.recent, weight, key_pos, cache_len,
                         self.evict_ws, self.kept, self.evict_status)
 

@@ -23,14 +23,16 @@ def score(cap=0.0, slopes=None, key_pos=None, root_pos=None):
 
 def test_scored_attention():
     L = B.lib()
-    at = lambda sh=shape(), sc=score(), q=ONE, lse=ONE, m=4096, ws=ONE, wsb=1 << 30: L.s4c_tree_attn_scored(
-        C.byref(sh), sc, q, ONE, ONE, ONE, ONE, ONE, ONE, m, 0.0, ONE, lse, None, ws, wsb, None)
+    at = lambda sh=shape(), sc=score(), q=ONE, lse=ONE, m=4096, ws=ONE, wsb=1 << 30, scale=0.0: L.s4c_tree_attn_scored(
+        C.byref(sh), sc, q, ONE, ONE, ONE, ONE, ONE, ONE, m, scale, ONE, lse, None, ws, wsb, None)
     assert at(q=None) == -1 and at(sh=shape(N=129)) == -3 and at(sh=shape(Hq=7)) == -2 and at(m=1 << 20) == -2
     assert at(q=C.c_void_p(264)) == -2
     assert B.s4c_tree_attn_workspace_size(shape(), 4096) > 0 and at(ws=None) == -4 and at(wsb=8) == -4
     for cap in (-1.0, float("nan"), float("inf"), -float("inf"), 3.3e38, 1e-40, 1e28, 1e-28):
         assert at(sc=score(cap)) == -2, cap
     assert at(sc=score(0.0, ONE, ONE, None)) == -1
+    for scale in (1e-19, 1e19):
+        assert at(sc=score(0.0, ONE), scale=scale) == -2, scale
     pg = lambda sh=shape(), bt=ONE, mb=64, ps=128, npg=200, pool=ONE: L.s4c_tree_attn_scored_paged(
         C.byref(sh), score(), ONE, ONE, ONE, pool, ONE, bt, mb, ps, npg, ONE, ONE, 4096, 0.0, ONE, None, None, ONE, 1 << 30, None)
     assert pg(bt=None) == -1 and pg(pool=None) == -1 and pg(ps=96) == -3 and pg(mb=0) == -2 and pg(npg=0) == -2 and pg(mb=63) == -2

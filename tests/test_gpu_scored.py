@@ -155,6 +155,21 @@ def test_caps_at_the_ends_of_their_range(N):
         c.check(c.score(cap, "none"))
 
 
+@pytest.mark.parametrize("N,bias", [(7, "none"), (80, "none"), (80, "rows")])
+def test_capped_scores_whose_squares_are_not_finite(N, bias):
+    """Scores of 2^69 k, k = 0 .. 4, and one of 2^72, the cap; every other row's weight is 0 and the output that one row's value."""
+    c = Case(15, 1, N, 4, 2, 128, "bf16", (256,), 256)
+    c.q.zero_()
+    c.q[..., 0] = 2.0 ** 35
+    c.kt.zero_()
+    c.kc.zero_()
+    c.kc[:, :, :, 0] = 2.0 ** 34 * (torch.arange(256, device="cuda") % 5).to(torch.bfloat16)
+    c.kc[:, :, 100, 0] = 2.0 ** 37
+    c.call(c.score(2.0 ** 72, bias), scale=1.0)
+    c.check(c.score(2.0 ** 72, bias), scale=1.0)
+    assert torch.equal(c.out, c.vc[:, None, :, 100].repeat_interleave(2, 2).expand(1, N, 4, 128))
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_random_shapes(seed):
     r = np.random.default_rng([seed, 5])

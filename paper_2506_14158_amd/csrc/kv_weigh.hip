@@ -7,8 +7,9 @@
 // in operand order, and the scores come out with a lane per key, so that a key's sum over the rows is additions in registers and two
 // exchanges between the wave's quarters.  No workgroup needs another's result, every sum has one order.
 // Measured: 16 x 64/8 heads, 32768 keys, 7 path nodes 214 us (1.1 GB at 5.2 TB/s); 8 x 32/8 heads, 6150 keys on average, paged 23.5 (4.5 TB/s); 32 heads,
-// 1029 keys 6, a chain of latencies: lengths, path, query rows.  With many query rows (512 of them, 4096 keys, 16 KV heads: 22.5 us) the exponentials
-// bound it.
+// 1029 keys 6, a chain of latencies: lengths, path, query rows.  With many query rows (512 of them, 4096 keys, 16 KV heads: 19.6 us) it is
+// bound by what a block of them goes through, LDS, matrix cores, exponentials, and by the start: about 2.7 us for 128 rows and 5 us.  (Multiplying the next block
+// while the exponentials of one are taken changed nothing.)
 #include "attn_score.h"
 
 namespace s4c {
@@ -18,7 +19,9 @@ namespace {
 using namespace mfma;
 using parts::u32x4;                          // (arrays of HIP's uint4 are not kept in registers)
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+// Many query rows (below) of 16 bits are shared by eight waves, so that half as many are read and written to LDS: 2 x 8 KV heads, 4096 keys, 512 rows 23.1 and
+// 19.6 us; 4 x 8, 20000 keys, 400 rows 133 and 115; 16 x 8, 6000 keys, 168 rows 90 and 79.  Of fp32, with twice the registers a row, by four (64 us; 69).
+constexpr int waves_of(bool many, size_t element) { return many && element == 2 ? 8 : 4; }
 // 16-byte pieces of a row that a lane has: piece 4 t + lane / 16 of its row for t < T.
 template <typename E, int D, int NG>
 struct Tile {
@@ -41,7 +44,8 @@ __device__ __forceinline__ f32x4 product(u32x4 q, u32x4 k, f32x4 c) {
 // MANY: the path may have more query rows than lie in LDS at a time.  Then these are replaced while the matrix cores work, chunk by chunk for
 // every tile of keys (two buffers, one barrier a chunk).
 template <typename E, int D, int NG, bool PAGED, bool MANY>
-__global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
+__global__ __launch_bounds__(64 * waves_of(MANY, sizeof(E)), 2) void kv_weigh_kernel(WeighArgs a) {
+    constexpr int kWaves = waves_of(MANY, sizeof(E)), kThreads = 64 * kWaves;
     typedef Tile<E, D, NG> T;
     constexpr int kBufs = MANY ? 2 : 1, kTogether = MANY ? 2 : 1;       // blocks of 16 rows at a time
     __shared__ __attribute__((aligned(16))) unsigned char s_q[kBufs][T::kRows * T::kRowB];     // [16-row block][piece t][lane] 16 bytes
@@ -263,6 +267,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_weigh_kernel(WeighArgs a) {
 
 template <typename E, int D, int NG, bool MANY>
 hipError_t launch(const WeighArgs& a, int per_cu, hipStream_t st) {
+    constexpr int kWaves = waves_of(MANY, sizeof(E)), kThreads = 64 * kWaves;
     const int units = a.B * a.Hkv, step = kWaves * 16 * NG, steps = (a.max_cache_len + step - 1) / step;
     int runs = (per_cu * a.cus + units - 1) / units;
     if (runs > steps) runs = steps;
@@ -273,11 +278,12 @@ hipError_t launch(const WeighArgs& a, int per_cu, hipStream_t st) {
 }
 // Tiles of half as many keys, four workgroups for a CU (three of which run at a time), unless there are many keys: then whole tiles, two workgroups
 // for a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and 11.2; 128 x
-// 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).  Where query rows are replaced, which takes registers, half ones.
+// 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).  Where query rows are replaced, which takes registers, half
+// ones, and one workgroup of eight waves for a CU (4 x 8 KV heads, 20000 keys, 400 rows: two 118, one 115).
 template <typename E, int D, int NG>
 hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
-    const long long step = kWaves * 16 * NG, steps = (long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step);
-    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, 4, st);
+    const long long step = waves_of(false, sizeof(E)) * 16 * NG, steps = (long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step);
+    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, waves_of(true, sizeof(E)) == 8 ? 1 : 4, st);
     if (steps <= 16ll * a.cus) return launch<E, D, NG / 2, false>(a, 4, st);
     return launch<E, D, NG, false>(a, 2, st);
 }

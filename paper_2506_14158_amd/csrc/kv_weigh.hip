@@ -10,6 +10,8 @@
 // 1029 keys 6, a chain of latencies: lengths, path, query rows.  With many query rows (512 of them, 4096 keys, 16 KV heads: 19.6 us) it is
 // bound by what a block of them goes through, LDS, matrix cores, exponentials, and by the start: about 2.7 us for 128 rows and 5 us.  (Multiplying the next block
 // while the exponentials of one are taken changed nothing.)
+#include <algorithm>
+
 #include "attn_score.h"
 
 namespace s4c {
@@ -20,7 +22,8 @@ using namespace mfma;
 using parts::u32x4;                          // (arrays of HIP's uint4 are not kept in registers)
 
 // Many query rows (below) of 16 bits are shared by eight waves, so that half as many are read and written to LDS: 2 x 8 KV heads, 4096 keys, 512 rows 23.1 and
-// 19.6 us; 4 x 8, 20000 keys, 400 rows 133 and 115; 16 x 8, 6000 keys, 168 rows 90 and 79.  Of fp32, with twice the registers a row, by four (64 us; 69).
+// 19.6 us; 4 x 8, 20000 keys, 400 rows 133 and 115; 16 x 8, 6000 keys, 168 rows 90 and 79.  Of fp32, with twice the registers a row, by four (8 x 6000
+// keys, 400 rows 64 us; 69).
 constexpr int waves_of(bool many, size_t element) { return many && element == 2 ? 8 : 4; }
 // 16-byte pieces of a row that a lane has: piece 4 t + lane / 16 of its row for t < T.
 template <typename E, int D, int NG>
@@ -47,7 +50,7 @@ template <typename E, int D, int NG, bool PAGED, bool MANY>
 __global__ __launch_bounds__(64 * waves_of(MANY, sizeof(E)), 2) void kv_weigh_kernel(WeighArgs a) {
     constexpr int kWaves = waves_of(MANY, sizeof(E)), kThreads = 64 * kWaves;
     typedef Tile<E, D, NG> T;
-    constexpr int kBufs = MANY ? 2 : 1, kTogether = MANY ? 2 : 1;       // blocks of 16 rows at a time
+    constexpr int kBufs = MANY ? 2 : 1, kTogether = MANY && NG < 4 ? 2 : 1;      // blocks of 16 rows at a time
     __shared__ __attribute__((aligned(16))) unsigned char s_q[kBufs][T::kRows * T::kRowB];     // [16-row block][piece t][lane] 16 bytes
     __shared__ __attribute__((aligned(16))) float s_lse[kBufs][T::kRows], s_slope[kBufs][T::kRows];
     __shared__ int s_node[kBufs][T::kRows];
@@ -266,26 +269,46 @@ __global__ __launch_bounds__(64 * waves_of(MANY, sizeof(E)), 2) void kv_weigh_ke
 }
 
 template <typename E, int D, int NG, bool MANY>
-hipError_t launch(const WeighArgs& a, int per_cu, hipStream_t st) {
-    constexpr int kWaves = waves_of(MANY, sizeof(E)), kThreads = 64 * kWaves;
-    const int units = a.B * a.Hkv, step = kWaves * 16 * NG, steps = (a.max_cache_len + step - 1) / step;
-    int runs = (per_cu * a.cus + units - 1) / units;
-    if (runs > steps) runs = steps;
-    const dim3 grid((unsigned)units, (unsigned)runs);
-    if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true, MANY>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false, MANY>), grid, dim3(kThreads), 0, st, a);
+hipError_t launch(const WeighArgs& a, int runs, hipStream_t st) {
+    const dim3 grid((unsigned)(a.B * a.Hkv), (unsigned)runs), block(64 * waves_of(MANY, sizeof(E)));
+    if (a.block_table) hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, true, MANY>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_weigh_kernel<E, D, NG, false, MANY>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-// Tiles of half as many keys, four workgroups for a CU (three of which run at a time), unless there are many keys: then whole tiles, two workgroups
-// for a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and 11.2; 128 x
-// 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).  Where query rows are replaced, which takes registers, half
-// ones, and one workgroup of eight waves for a CU (4 x 8 KV heads, 20000 keys, 400 rows: two 118, one 115).
+// Few query rows: tiles of half as many keys, four workgroups for a CU (three of which run at a time), unless there are many keys: then whole tiles,
+// two workgroups for a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and
+// 11.2; 128 x 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).
+// Many, 16 bits: whole tiles, which read the query rows from LDS half as often, where they fill the chip (units x keys, rows, whole and half, us: 8 x 8192,
+// 512 29.4 and 19.8; 8 x 16384, 512 31.3 and 33.3; 16 x 16384, 512 54.2 and 58.8; 128 x 2000, 168 28.8 and 31.6; 128 x 6000, 168 70 and 79; 32 x 20000,
+// 400 100 and 110).  One workgroup of eight waves runs on a CU at a time, so one more than CUs would take as long as twice as many (24 x 16384, 512: 264
+// 124 us, 240 92; 320 x 4000, 168: 320 206, 640 146).
 template <typename E, int D, int NG>
 hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
-    const long long step = waves_of(false, sizeof(E)) * 16 * NG, steps = (long long)a.B * a.Hkv * ((a.max_cache_len + step - 1) / step);
-    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) return launch<E, D, NG / 2, true>(a, waves_of(true, sizeof(E)) == 8 ? 1 : 4, st);
-    if (steps <= 16ll * a.cus) return launch<E, D, NG / 2, false>(a, 4, st);
-    return launch<E, D, NG, false>(a, 2, st);
+    const long long units = (long long)a.B * a.Hkv;
+    auto steps = [&](long long step) { return (a.max_cache_len + step - 1) / step; };
+    auto runs = [&](int per_cu, long long n) { return (int)std::min((per_cu * a.cus + units - 1) / units, n); };
+    if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) {
+        constexpr int kWaves = waves_of(true, sizeof(E));
+        const long long whole = steps(kWaves * 16 * NG), half = steps(kWaves * 8 * NG);
+        if constexpr (kWaves == 8) {
+            auto shared_out = [&](long long n) {                         // n steps a unit -> runs; the start of a run takes as long as a step
+                const long long least_turns = (units + a.cus - 1) / a.cus;
+                long long best = 1, least = 0;
+                for (long long turns = least_turns; turns < least_turns + 4; ++turns) {
+                    const long long most = std::min(turns * a.cus / units, n), cost = turns * ((n + most - 1) / most + 1);
+                    if (least == 0 || cost < least) { least = cost; best = most; }
+                }
+                return (int)best;
+            };
+            return units * whole >= a.cus ? launch<E, D, NG, true>(a, shared_out(whole), st) : launch<E, D, NG / 2, true>(a, shared_out(half), st);
+        } else {
+            return launch<E, D, NG / 2, true>(a, runs(4, half), st);
+        }
+    }
+    constexpr int kWaves = waves_of(false, sizeof(E));
+    const long long whole = steps(kWaves * 16 * NG);
+    if (units * whole <= 16ll * a.cus) return launch<E, D, NG / 2, false>(a, runs(4, steps(kWaves * 8 * NG)), st);
+    return launch<E, D, NG, false>(a, runs(2, whole), st);
 }
 
 }  // namespace

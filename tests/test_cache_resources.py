@@ -4,7 +4,7 @@ import pytest
 from tests.test_resources import resources
 
 
-@pytest.mark.parametrize("source,kernels", [("kv_weigh.hip", 36), ("kv_evict.hip", 17)])
+@pytest.mark.parametrize("source,kernels", [("kv_weigh.hip", 44), ("kv_evict.hip", 17)])
 def test_nothing_spills(source, kernels):
     found = resources(source)
     assert len(found) == kernels

@@ -118,6 +118,20 @@ def test_weights_against_the_definition(name, dtype):
         assert torch.equal(c.win[b, :, :n], c.w[b, :, :n]) and torch.equal(c.win[b, :, n:], before[b, :, n:])
 
 
+@pytest.mark.parametrize("D,dtype,top,page", [(64, "bf16", 1100, 0), (128, "f16", 300, 0), (128, "bf16", 576, 64), (64, "f16", 256, 128)])
+def test_weights_of_many_query_rows_and_units(D, dtype, top, page):
+    """Enough (sequence, KV head)s for the larger tiles, lengths on both sides of them, one to three steps."""
+    lengths = [top, 45, 64, 200, top // 2, 129, top - 1, 255]
+    c = Weigh(70 + D, 8, 43, 128, 32, D, dtype, lengths, (42, 3, 42, 40, 42, 0, 42, 33), top, page)
+    for cap, bias in ((0.0, "none"), (8.0, "kept"), (0.0, "rows")):
+        s = c.score(cap, bias)
+        want = c.want(s)
+        before = c.w.fill_(7.0).clone()
+        c.call(s)
+        assert not c.status.any()
+        c.check(s, want, c.w, before)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_weights_of_random_shapes(seed):
     r = np.random.default_rng([seed, 6])

@@ -276,39 +276,40 @@ hipError_t launch(const WeighArgs& a, int runs, hipStream_t st) {
     return hipGetLastError();
 }
 // Few query rows: tiles of half as many keys, four workgroups for a CU (three of which run at a time), unless there are many keys: then whole tiles,
-// two workgroups for a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and
+// two workgroups on a CU, each with a longer run (bf16, head size 128, units x keys, whole and half tiles, us: 32 x 1029 7.7 and 6.3; 160 x 1000 13.7 and
 // 11.2; 128 x 2000 17.9 and 16.3; 128 x 8000 58.4 and 56.7; 128 x 32768 208 and 216).
 // Many, 16 bits: whole tiles, which read the query rows from LDS half as often, where they fill the chip (units x keys, rows, whole and half, us: 8 x 8192,
 // 512 29.4 and 19.8; 8 x 16384, 512 31.3 and 33.3; 16 x 16384, 512 54.2 and 58.8; 128 x 2000, 168 28.8 and 31.6; 128 x 6000, 168 70 and 79; 32 x 20000,
-// 400 100 and 110).  One workgroup of eight waves runs on a CU at a time, so one more than CUs would take as long as twice as many (24 x 16384, 512: 264
-// 124 us, 240 92; 320 x 4000, 168: 320 206, 640 146).
+// 400 100 and 110).  One workgroup of eight waves runs on a CU at a time.
+// Where workgroups run long, one more than run at a time takes as long as twice as many: runs are chosen by the turns they take (units x keys, rows, workgroups,
+// us: 24 x 16384, 512: 264 124, 240 92; 320 x 4000, 168: 320 206, 640 146; whole tiles of few rows: 72 x 16000: 576 71, 504 61; 160 x 16000: 640 142,
+// 480 133; 520 x 3000: 520 105, 1560 91).
 template <typename E, int D, int NG>
 hipError_t launch_tiles(const WeighArgs& a, hipStream_t st) {
     const long long units = (long long)a.B * a.Hkv;
     auto steps = [&](long long step) { return (a.max_cache_len + step - 1) / step; };
     auto runs = [&](int per_cu, long long n) { return (int)std::min((per_cu * a.cus + units - 1) / units, n); };
+    auto shared_out = [&](long long at_once, long long n) {           // n steps a unit -> runs; the start of a run takes as long as a step
+        const long long least_turns = (units + at_once - 1) / at_once;
+        long long best = 1, least = 0;
+        for (long long turns = least_turns; turns < least_turns + 4; ++turns) {
+            const long long most = std::min(turns * at_once / units, n), cost = turns * ((n + most - 1) / most + 1);
+            if (least == 0 || cost < least) { least = cost; best = most; }
+        }
+        return (int)best;
+    };
     if ((long long)a.max_path * a.G > Tile<E, D, NG>::kRows) {
         constexpr int kWaves = waves_of(true, sizeof(E));
         const long long whole = steps(kWaves * 16 * NG), half = steps(kWaves * 8 * NG);
-        if constexpr (kWaves == 8) {
-            auto shared_out = [&](long long n) {                         // n steps a unit -> runs; the start of a run takes as long as a step
-                const long long least_turns = (units + a.cus - 1) / a.cus;
-                long long best = 1, least = 0;
-                for (long long turns = least_turns; turns < least_turns + 4; ++turns) {
-                    const long long most = std::min(turns * a.cus / units, n), cost = turns * ((n + most - 1) / most + 1);
-                    if (least == 0 || cost < least) { least = cost; best = most; }
-                }
-                return (int)best;
-            };
-            return units * whole >= a.cus ? launch<E, D, NG, true>(a, shared_out(whole), st) : launch<E, D, NG / 2, true>(a, shared_out(half), st);
-        } else {
+        if constexpr (kWaves == 8)
+            return units * whole >= a.cus ? launch<E, D, NG, true>(a, shared_out(a.cus, whole), st) : launch<E, D, NG / 2, true>(a, shared_out(a.cus, half), st);
+        else
             return launch<E, D, NG / 2, true>(a, runs(4, half), st);
-        }
     }
     constexpr int kWaves = waves_of(false, sizeof(E));
     const long long whole = steps(kWaves * 16 * NG);
     if (units * whole <= 16ll * a.cus) return launch<E, D, NG / 2, false>(a, runs(4, steps(kWaves * 8 * NG)), st);
-    return launch<E, D, NG, false>(a, runs(2, whole), st);
+    return launch<E, D, NG, false>(a, shared_out(2 * a.cus, whole), st);
 }
 
 }  // namespace

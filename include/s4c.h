@@ -355,7 +355,8 @@ typedef struct {
  *   score  host pointer, nullable (nothing changed)
  *   lse    [B][N][Hq] fp32 nullable: natural log of the sum of exp(changed score) over the keys that the row sees; +infinity for
  *          the rows of a flagged sequence.
- * Scores and statistics are fp32 (a cap's tanh is off by less than 2^-22 of itself).  Results are deterministic. */
+ * Scores and statistics are fp32 (a cap's tanh is off by less than 2^-22 of itself).  As in s4c_tree_attn, values are summed up in fp32 times
+ * exponentials of 2^8 at most: the largest |V| times the number of keys has to lie below 2^119.  Results are deterministic. */
 s4c_status s4c_tree_attn_scored(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_tree,
                                 const void* v_tree, const void* k_cache, const void* v_cache, const int32_t* cache_len,
                                 const int32_t* parent, int32_t max_cache_len, float scale, void* out, float* lse, int32_t* status,

@@ -37,7 +37,10 @@ namespace {
 using namespace mfma;
 
 constexpr int kBN = 64;                     // keys per tile
-constexpr float kLazyLog2 = 8.0f;           // full tiles rescale only when a row maximum grew by more than 2^8
+// Full tiles rescale only when a row maximum grew by more than 2^8: sums of exponentials times values stay within 2^8 of the largest value
+// times the number of keys.  (With slopes the maximum grows from tile to tile; 2^64 there, in bf16: 16 x 64/8 heads, 32768 keys 2254 us and 2283, in order,
+// 2150 and 2154 looked up; 8 x 32/8 heads, 8192 keys 97 and 99, but an error of 1.73e-3 and 1.54e-3, and sums that overflow 2^56 earlier.)
+constexpr float kLazyLog2 = 8.0f;
 constexpr int lds_bytes_for(int ns, int d) { return ns * 2 * kBN * d * 2 + kMaxNodes * 16 + kMaxNodes * 4; }
 // with changed scores behind it: positions of the ring's keys, slopes of every wave's rows, depths of the nodes
 constexpr int scored_lds_bytes_for(int ns, int d, int wr) { return lds_bytes_for(ns, d) + ns * kBN * 4 + wr * 256 + kMaxNodes * 4; }
@@ -46,8 +49,6 @@ template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, 
 __global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
     constexpr bool kScored = SCORE != score::kPlain;
-    // Slopes make the largest score of a row grow from tile to tile, and bf16 has room for exponentials that are far above 1.
-    constexpr float kLag = !F16 && (SCORE == score::kSlopes || SCORE == score::kCapSlopes) ? 64.0f : kLazyLog2;
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row
@@ -448,7 +449,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             // consistent with whatever reference is current, which is all the final division (or the
             // merge of KV splits) needs.
             const float mt = kScored ? mx : mx * mul;
-            if (__any(mt > m_run + kLag)) {
+            if (__any(mt > m_run + kLazyLog2)) {
                 const float m_new = fmaxf(m_run, mt);
                 const float alpha = fast_exp2(m_run - m_new);          // first tile: exp2(-inf) = 0
                 l_run *= alpha;

@@ -13,8 +13,8 @@
 //   cap               C y p(y^2), y = x / cap, C = cap log2(e), p a fit of tanh(y)/y at Chebyshev nodes.  Where all scores of a wave are within 0.35
 //                     of the cap (and nothing is added), the kernel for many rows takes four terms (relative error 3.5e-8) with the scale in the
 //                     coefficients, and the last product is the one that makes the exponent: four more operations.  Within 0.6 five
-//                     terms (7.5e-8).  Beyond, C - 2 C / (1 + exp2(2 log2(e) y)), two more operations at a quarter of the rate, off by C 2^-23,
-//                     a relative 2.2e-7 there.
+//                     terms (7.5e-8).  Beyond, C - 2 C / (1 + exp2(2 log2(e) |y|)) with y's sign, two more operations at a quarter of the rate, off by
+//                     C 2^-23, a relative 2.2e-7 there.
 #pragma once
 #include "common.h"
 
@@ -39,9 +39,10 @@ __device__ __forceinline__ float fitted(float y, float c) {
     p = fmaf(z, p, kFit[0] * c);
     return y * p;
 }
+// (of |y|, and y's sign put back: below 0 the quotient would be the larger part of the result, with three times the rounding)
 __device__ __forceinline__ float beyond(float y, float c) {
-    const float e = fast_exp2(y * (2.f * kLog2e));       // infinity: the cap
-    return fmaf(-2.f * c, __builtin_amdgcn_rcpf(1.f + e), c);
+    const float e = fast_exp2(fabsf(y) * (2.f * kLog2e));       // infinity: the cap
+    return copysignf(fmaf(-2.f * c, __builtin_amdgcn_rcpf(1.f + e), c), y);
 }
 
 // products -> c tanh(to_y product) (cap > 0); N values, s(j) a reference to the j-th

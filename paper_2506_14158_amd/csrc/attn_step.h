@@ -23,14 +23,16 @@ struct StepTail {
 template <>
 struct StepTail<kNoStep> {};
 
-// The attention kernels' arguments, (AttnArgs, StepTail), read when they are asked for.  As the named parameters, all that the
-// whole kernel needs is loaded at its start and kept, and the attention's scalar registers do not hold it: a hundred values written
+// The attention kernels' arguments, (AttnArgs, StepTail) or, with changed scores, (ChangedAttnArgs, StepTail), read when they are asked for.
+// As the named parameters, all that the whole kernel needs is loaded at its start and kept, and the attention's scalar registers do not hold it: a hundred values written
 // to vector registers' lanes first, 0.2 us of every launch.
 struct Arguments {
     typedef const __attribute__((address_space(4))) unsigned char* Ptr;
     Ptr at;
     __device__ __forceinline__ Arguments() : at((Ptr)__builtin_amdgcn_kernarg_segment_ptr()) { asm volatile("" : "+s"(at)); }
     __device__ __forceinline__ const AttnArgs& attn() const { return *(const AttnArgs*)at; }
+    template <score::Kind SCORE>
+    __device__ __forceinline__ const score::Attn<SCORE>& attn() const { return *(const score::Attn<SCORE>*)at; }
     template <StepKind KIND>
     __device__ __forceinline__ const StepTail<KIND>& tail() const {
         constexpr size_t al = alignof(StepTail<KIND>);

@@ -215,6 +215,19 @@ struct Unchanged {};
 template <Kind KIND> struct ArgsOf { typedef Changed type; };
 template <> struct ArgsOf<kPlain> { typedef Unchanged type; };
 template <Kind KIND> using Args = typename ArgsOf<KIND>::type;
+constexpr bool biased(Kind kind) { return kind == kAny || kind == kSlopes || kind == kCapSlopes; }     // positions are asked for
+// An attention kernel's first argument: AttnArgs, and behind them what changes the scores.
+struct ChangedAttnArgs : AttnArgs {
+    Changed score;
+    ChangedAttnArgs(const AttnArgs& a, const Changed& sc) : AttnArgs(a), score(sc) {}
+};
+template <Kind KIND> struct AttnOf { typedef ChangedAttnArgs type; };
+template <> struct AttnOf<kPlain> { typedef AttnArgs type; };
+template <Kind KIND> using Attn = typename AttnOf<KIND>::type;
+inline AttnArgs with(const AttnArgs& a, const Unchanged&) { return a; }
+inline ChangedAttnArgs with(const AttnArgs& a, const Changed& sc) { return ChangedAttnArgs(a, sc); }
+__device__ __forceinline__ Unchanged of(const AttnArgs&) { return {}; }
+__device__ __forceinline__ const Changed& of(const ChangedAttnArgs& a) { return a.score; }
 }  // namespace score
 
 struct WeighArgs {

@@ -42,13 +42,28 @@ constexpr int kBN = 64;                     // keys per tile
 // 2150 and 2154 looked up; 8 x 32/8 heads, 8192 keys 97 and 99, but an error of 1.73e-3 and 1.54e-3, and sums that overflow 2^56 earlier.)
 constexpr float kLazyLog2 = 8.0f;
 constexpr int lds_bytes_for(int ns, int d) { return ns * 2 * kBN * d * 2 + kMaxNodes * 16 + kMaxNodes * 4; }
-// with changed scores behind it: positions of the ring's keys, slopes of every wave's rows, depths of the nodes
-constexpr int scored_lds_bytes_for(int ns, int d, int wr) { return lds_bytes_for(ns, d) + ns * kBN * 4 + wr * 256 + kMaxNodes * 4; }
+// with a bias behind it: positions of the ring's keys, slopes of every wave's rows, depths of the nodes
+constexpr int biased_lds_bytes_for(int ns, int d, int wr) { return lds_bytes_for(ns, d) + ns * kBN * 4 + wr * 256 + kMaxNodes * 4; }
+
+// Writes a row's log-sum-exp (score::Writer); its arguments are read when a row is done, the kernels have no registers left for them.
+template <score::Kind SCORE>
+struct LateWriter {
+    float shift;
+    __device__ __forceinline__ void operator()(size_t row, float m, float l) const { score::writer(score::of(Arguments().attn<SCORE>()), shift)(row, m, l); }
+};
+template <>
+struct LateWriter<score::kPlain> : work::NoRowDone {
+    __device__ __forceinline__ explicit LateWriter(float) {}
+};
 
 template <int WR, int NS, int WPE, bool PAGED, bool F16, int kD, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
-void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
-    constexpr bool kScored = SCORE != score::kPlain;
+void tree_attn_mfma_kernel(score::Attn<SCORE> a, StepTail<STEP> tail) {
+    constexpr bool kScored = SCORE != score::kPlain, kBiased = score::biased(SCORE);
+    constexpr bool kCapped = SCORE == score::kCap || SCORE == score::kCapSlopes;
+    const auto& sc = score::of(a);
+    // (what a segment or a rare tile asks for is read then)
+    auto late = []() __attribute__((always_inline)) -> const auto& { return score::of(Arguments().attn<SCORE>()); };
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row
@@ -63,7 +78,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     auto v_swz = [](int r) { return kD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
     constexpr int CH = (kBN * kD / 8) / NT;      // direct-to-LDS loads per thread per K (or V) tile
     static_assert(CH >= 1, "tile smaller than the workgroup");
-    constexpr int kLoads = 2 * CH + (kScored ? 1 : 0);       // of a wave and tile
+    constexpr int kLoads = 2 * CH + (kBiased ? 1 : 0);       // of a wave and tile
     static_assert(NS >= 2 && kLoads * (NS - 2) < 64, "too many loads in flight for vmcnt");
 
     static_assert(sizeof(accept::Shared) <= NS * kStageB, "the ring is also what the other workgroups of a step have");
@@ -77,7 +92,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     uint32_t* anc = (uint32_t*)(smem + NS * kStageB);        // [kMaxNodes][4]
     int32_t* spar = (int32_t*)(anc + kMaxNodes * 4);         // [kMaxNodes]
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
-    constexpr int kPosAt = lds_bytes_for(NS, kD), kSlopesAt = kPosAt + NS * kBN * 4;        // (changed scores)
+    constexpr int kPosAt = lds_bytes_for(NS, kD), kSlopesAt = kPosAt + NS * kBN * 4;        // (with a bias)
     int32_t* const ring_pos = (int32_t*)(smem + kPosAt);                         // [NS][kBN]
     float* const row_slopes = (float*)(smem + kSlopesAt);                        // [WR][64]
     float* const depths = (float*)(smem + kSlopesAt + WR * 256);                 // [kMaxNodes]
@@ -120,6 +135,23 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     const int rq = rq0 + (lane & 31);
     const bool rvalid = rq < M;
     const int node = rvalid ? rq / G : 0, g = rvalid ? rq - node * G : 0;
+    // This lane's row of the unit, its node and group head, and the lane's half of the wave.  Between the segments of a share they are found again, and
+    // arguments are read again: the kernels with changed scores and balanced shares have no registers to keep them, and what is made of
+    // them, while tiles are multiplied (up to five were in scratch memory).
+    constexpr bool kFindAgain = kScored && MERGE == parts::kShares;
+    auto args = [&]() __attribute__((always_inline)) -> const AttnArgs& {
+        if constexpr (kFindAgain) return Arguments().attn();
+        else return a;
+    };
+    struct Row { int r, node, g, half; };
+    auto my_row = [&]() __attribute__((always_inline)) {
+        if constexpr (!kFindAgain) return Row{rq, node, g, g32};
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        const AttnArgs& at = args();
+        const int r = min(rq0 + (l & 31), at.M - 1), nd = r / at.G;
+        return Row{r, nd, r - nd * at.G, l >> 5};
+    };
     size_t q_off[32 / kRPI];
     {
         // rows rq0 + kRPI c + lane / kLPR, one step of kRPI rows after the other; past the last row: the last
@@ -136,6 +168,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             if (gg >= G) { gg -= G; ++nd; }
         }
     }
+    const LateWriter<SCORE> row_done{kShift};
     if constexpr (MERGE == parts::kHere)
         if (wave == 0) parts::begin<kD>(a, team, mt);
     constexpr bool kOne = MERGE != parts::kShares;        // a share is one segment
@@ -148,7 +181,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         }
         if constexpr (MERGE == parts::kHere || MERGE == parts::kNext)
             if (work::leaves_empty(a, team))
-                parts::finish<kD, kElem, MERGE, WR, WR>(a, team, mt, smem, [&]() __attribute__((always_inline)) { parts::put_empty<kD, 1, MERGE>(a, team, mt * WR + wave, 0); }, score::writer(sc, kShift));
+                parts::finish<kD, kElem, MERGE, WR, WR>(a, team, mt, smem, [&]() __attribute__((always_inline)) { parts::put_empty<kD, 1, MERGE>(a, team, mt * WR + wave, 0); }, row_done);
         lens_end<STEP>(lens_look_back<STEP>());
         return;
     }
@@ -173,19 +206,19 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
                        ((((size_t)id * a.Hkv + pw.kvh) << a.page_shift) + (size_t)(k0 & ((1 << a.page_shift) - 1))) * kRowB);
     };
     auto begin_segment = [&]() __attribute__((always_inline)) {
-        p_full = uniform(max(0, min(work::usable(a, lens.at(a, pw.b)) / kBN, pw.tile_end) - pw.tile));
+        p_full = uniform(max(0, min(work::usable(args(), lens.at(args(), pw.b)) / kBN, pw.tile_end) - pw.tile));
         p_key = pw.tile * kBN;
         if constexpr (!PAGED)
-            p_k = uniform((const unsigned char*)a.k_cache + (((size_t)pw.b * a.Hkv + pw.kvh) * (size_t)a.S_cap + p_key) * kRowB);
+            p_k = uniform((const unsigned char*)args().k_cache + (((size_t)pw.b * args().Hkv + pw.kvh) * (size_t)args().S_cap + p_key) * kRowB);
     };
     begin_segment();
     auto stage_base = [&]() __attribute__((always_inline)) {
         return __builtin_amdgcn_readfirstlane(lds0 + ((uint32_t)issued % NS) * kStageB + wave * 1024);
     };
-    // The positions of the tile's keys, from key k0 on (changed scores; where they are not looked up something that is not used,
+    // The positions of the tile's keys, from key k0 on (with a bias; where they are not looked up something that is not used,
     // so that the loads in flight are as many).  Every wave loads them all: each counts loads of its own.
     auto issue_pos = [&](int k0, int last, const unsigned char* otherwise) __attribute__((always_inline)) {
-        if constexpr (kScored) {
+        if constexpr (kBiased) {
             const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + kPosAt + ((uint32_t)issued % NS) * (kBN * 4));
             const unsigned char* p = otherwise ? otherwise : (const unsigned char*)(sc.key_pos + ((size_t)pw.b * a.Hkv + pw.kvh) * (size_t)a.S_cap + k0);
             dma4(p + 4 * min(lane, last), at);
@@ -200,13 +233,13 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             dma16(kg, kvo_k[c], sbase + WR * c * 1024);
             dma16(vg, kvo_v[c], sbase + WR * c * 1024 + kTileB);
         }
-        if constexpr (kScored) issue_pos(p_key, kBN - 1, sc.key_pos ? nullptr : kg);
-        if constexpr (PAGED || kScored) p_key += kBN;
+        if constexpr (kBiased) issue_pos(p_key, kBN - 1, sc.key_pos ? nullptr : kg);
+        if constexpr (PAGED || kBiased) p_key += kBN;
         if constexpr (!PAGED) p_k += kBN * kRowB;
     };
     auto end_tile = [&]() __attribute__((always_inline)) {
         if (pw.tile == pw.tile_end) {
-            if constexpr (kOne) pw.b = -1; else pw = work::walk_next(a, lens, pw);
+            if constexpr (kOne) pw.b = -1; else pw = work::walk_next(args(), lens, pw);
             if (!kOne && pw.b >= 0) begin_segment();
         }
     };
@@ -216,17 +249,17 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             issue_full();
             --p_full;
         } else {
-            const int P = work::usable(a, lens.at(a, pw.b)), u_pref = (P + kBN - 1) / kBN;
+            const int P = work::usable(args(), lens.at(args(), pw.b)), u_pref = (P + kBN - 1) / kBN;
             const uint32_t sbase = stage_base();
             const bool tree = pw.tile > u_pref;
             const int k0 = (pw.tile - 1 - (tree ? u_pref : 0)) * kBN;
             const unsigned char* kg;
-            if (tree) kg = uniform((const unsigned char*)a.k_tree + (((size_t)pw.b * N + k0) * a.Hkv + pw.kvh) * kRowB);
+            if (tree) kg = uniform((const unsigned char*)args().k_tree + (((size_t)pw.b * N + k0) * args().Hkv + pw.kvh) * kRowB);
             else kg = PAGED ? page_addr(k0) : uniform(p_k);
             kg = uniform(kg);
-            const unsigned char* vg = uniform(kg + (tree ? vt_minus_kt : v_minus_k));
+            const unsigned char* vg = uniform(kg + (!tree ? v_minus_k : kFindAgain ? (const unsigned char*)args().v_tree - (const unsigned char*)args().k_tree : vt_minus_kt));
             const int last = (tree ? N : P) - 1 - k0;                       // >= 0: last valid row of the tile
-            const uint32_t rstride = tree ? tree_stride : (uint32_t)kRowB;
+            const uint32_t rstride = !tree ? (uint32_t)kRowB : kFindAgain ? (uint32_t)args().Hkv * kRowB : tree_stride;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int row = kRPI * (wave + WR * c) + lane / kLPR, pc = lane % kLPR;
@@ -234,7 +267,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
                 dma16(kg, roff + ((pc ^ k_swz(row)) << 4), sbase + WR * c * 1024);
                 dma16(vg, roff + ((pc ^ v_swz(row)) << 4), sbase + WR * c * 1024 + kTileB);
             }
-            if constexpr (kScored) issue_pos(k0, last, sc.key_pos && !tree ? nullptr : kg);
+            if constexpr (kBiased) issue_pos(k0, last, sc.key_pos && !tree ? nullptr : kg);
         }
         ++issued;
         end_tile();
@@ -255,7 +288,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
 #pragma unroll
         for (int c = 0; c < 32 / kRPI; ++c) dma16(qb + q_off[c], __builtin_amdgcn_readfirstlane(lds0 + q_stage + c * 1024));
     }
-    if constexpr (kScored)
+    if constexpr (kBiased)
         if (sc.slopes) dma4(sc.slopes + cw.kvh * G + g, __builtin_amdgcn_readfirstlane(lds0 + kSlopesAt + wave * 256));
     for (int t = 0; t < NS - 2 && t < n_share; ++t) issue_next();
     if (issued == NS - 2) wait_vmcnt<kLoads * (NS - 2)>(); else wait_vmcnt<0>();
@@ -270,7 +303,8 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         qf[t] = __builtin_bit_cast(bf16x8, raw);
     }
     auto load_q = [&](int b, int kvh) __attribute__((always_inline)) {
-        const bf16_t* qrow = (const bf16_t*)a.q + (((size_t)b * N + node) * a.Hq + kvh * G + g) * kD + g32 * 8;
+        const Row row = my_row();
+        const bf16_t* qrow = (const bf16_t*)args().q + (((size_t)b * args().N + row.node) * args().Hq + kvh * args().G + row.g) * kD + row.half * 8;
 #pragma unroll
         for (int t = 0; t < kKT; ++t) {
             uint4 raw = make_uint4(0, 0, 0, 0);
@@ -285,35 +319,37 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     while (issued < NS - 1 && issued < n_share) issue_next();
 
     float slope = 0.f;                                    // of this lane's row, in units of the scores before sc.mul
-    if constexpr (kScored)
-        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * sc.slope_mul;
+    if constexpr (kBiased)
+        if (sc.slopes) slope = row_slopes[wave * 64 + lane] * late().slope_mul;
     int parent = -1, b_known = cw.b;
     bool masks = false;                                   // anc[] holds b_known's masks
     while (cw.b >= 0) {
     const int b = cw.b, kvh = cw.kvh;
-    const int P = work::usable(a, lens.at(a, b)), u_pref = (P + kBN - 1) / kBN, t_end = uniform(cw.tile_end);
+    const int P = work::usable(args(), lens.at(args(), b)), u_pref = (P + kBN - 1) / kBN, t_end = uniform(cw.tile_end);
     if (b != b_known) {
         b_known = b;
         masks = false;
-        len_bad = P != lens.at(a, b);
-        if constexpr (PAGED) len_bad = len_bad || work::pages_are_bad(a, b, P);
+        len_bad = P != lens.at(args(), b);
+        if constexpr (PAGED) len_bad = len_bad || work::pages_are_bad(args(), b, P);
         __syncthreads();                                  // the previous sequence's parent[] is no longer read
         if (tid < N) spar[tid] = parent;
         __syncthreads();
     }
     uint32_t amask[4] = {0, 0, 0, 0};
+    auto read_masks = [&]() __attribute__((always_inline)) {
+        if (!rvalid) return;
+        const uint4 m = *(const uint4*)(anc + my_row().node * 4);
+        amask[0] = m.x; amask[1] = m.y; amask[2] = m.z; amask[3] = m.w;
+    };
     if (t_end > u_pref) {
         if (!masks) {
             if (!work::tree_is_bad(a, spar)) work::build_masks(a, spar, anc);
             else if (tid < N) *(uint4*)(anc + tid * 4) = make_uint4(0, 0, 0, 0);
-            if constexpr (kScored) score::note_depth(a, anc, depths);
+            if constexpr (kBiased) score::note_depth(a, anc, depths);
             __syncthreads();
             masks = true;
         }
-        if (rvalid) {
-            const uint4 m = *(const uint4*)(anc + node * 4);
-            amask[0] = m.x; amask[1] = m.y; amask[2] = m.z; amask[3] = m.w;
-        }
+        if constexpr (!kScored) read_masks();
     }
 
     f32x16 o[kDB];
@@ -323,9 +359,9 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;      // l_run: this lane's half of the keys only
     int root = 0;                              // position of the root, where positions are looked up
-    if constexpr (kScored)
-        if (sc.key_pos) root = scalar_load_i32(uniform((const unsigned char*)sc.root_pos), (uint32_t)uniform(b) * 4u);
-    int key0 = 0;                              // the tile's first key (for changed scores)
+    if constexpr (kBiased)
+        if (sc.key_pos) root = scalar_load_i32(uniform((const unsigned char*)late().root_pos), (uint32_t)uniform(b) * 4u);
+    int key0 = 0;                              // the tile's first key (for a bias)
 
     // ---- one tile: scores, (mask,) online softmax, accumulate
     // kTail: keys >= arg masked; kTree: tree tile `arg` of the unit, ancestor mask
@@ -333,11 +369,11 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         constexpr int MODE = decltype(mode_tag)::value;
         const lds_u8* stage = (const lds_u8*)smem + ((uint32_t)done % NS) * kStageB;     // LDS address space throughout
 
-        // key lane % 32 of a block, from the root (changed scores)
+        // key lane % 32 of a block, from the root (for a bias)
         auto distance = [&](int kblk) __attribute__((always_inline)) {
             const int in = 32 * kblk + (lane & 31);
             if constexpr (MODE == kTree) return depths[arg * kBN + in];
-            else if constexpr (kScored) {
+            else if constexpr (kBiased) {
                 const int p = ring_pos[((uint32_t)done % NS) * kBN + in];
                 return (float)(sc.key_pos ? p - root : key0 + in - P);
             } else return 0.f;
@@ -385,11 +421,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         }
 
         // ---- changed scores
-        float mul = a.scale_log2;                             // to log2 units
+        const float mul = kCapped ? 1.f : a.scale_log2;       // to log2 units
         bool fits = false;
         if constexpr (kScored) {
-            mul = sc.mul;
-            if constexpr (SCORE == score::kCap || SCORE == score::kCapSlopes) {
+            if constexpr (kCapped) {
                 if constexpr (MODE == kPlain) {
                     float most = fmaxf(fabsf(s[0][0]), fabsf(s[1][0]));
 #pragma unroll
@@ -397,9 +432,10 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
                     fits = !__any(most > sc.fit_up_to);
                 }
                 if (MODE != kPlain || __builtin_expect(!fits, 0)) {
-                    const float c = MODE == kPlain ? 1.f : sc.cap_log2;
-                    score::cap(s[0], sc, c);
-                    score::cap(s[1], sc, c);
+                    const auto& changed = late();
+                    const float c = MODE == kPlain ? 1.f : changed.cap_log2;
+                    score::cap(s[0], changed, c);
+                    score::cap(s[1], changed, c);
                 }
             }
             if constexpr (SCORE == score::kCapSlopes) {
@@ -538,7 +574,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     // vmcnt wait of its own inside the tile loop.
 #pragma unroll
     for (int t = 0; t < kKT; ++t) asm volatile("" : "+v"(qf[t]));
-    if constexpr (kScored) asm volatile("" : "+v"(slope));
+    if constexpr (kBiased) asm volatile("" : "+v"(slope));
 
     auto sync = [&]() __attribute__((always_inline)) {
         // tile `done` has landed once at most NS-2 younger tiles of this wave are outstanding
@@ -555,7 +591,7 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             __syncthreads();
             issue_full();
             ++issued;
-            if constexpr (kScored) key0 = (t + i) * kBN;
+            if constexpr (kBiased) key0 = (t + i) * kBN;
             if (wave_on) tile_body(std::integral_constant<int, kPlain>{}, 0);
         }
         t += n;
@@ -565,14 +601,16 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
     }
     for (const int e = min(P / kBN, t_end); t < e; ++t, ++done) {
         sync();
-        if constexpr (kScored) key0 = t * kBN;
+        if constexpr (kBiased) key0 = t * kBN;
         if (wave_on) tile_body(std::integral_constant<int, kPlain>{}, 0);
     }
     for (const int e = min(u_pref, t_end); t < e; ++t, ++done) {
         sync();
-        if constexpr (kScored) key0 = t * kBN;
+        if constexpr (kBiased) key0 = t * kBN;
         if (wave_on) tile_body(std::integral_constant<int, kTail>{}, P - t * kBN);
     }
+    if constexpr (kScored)                                // (four registers more for the tiles before)
+        if (t < t_end) read_masks();
     for (; t < t_end; ++t, ++done) {
         sync();
         if (wave_on) tile_body(std::integral_constant<int, kTree>{}, t - u_pref);
@@ -580,18 +618,20 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
 
     work::Walk nw = cw;
     if constexpr (!kOne) {
-        nw = work::walk_next(a, lens, cw);
+        nw = work::walk_next(args(), lens, cw);
         if (nw.b >= 0) {
-            if (nw.b != b && tid < N) parent = a.parent[(size_t)nw.b * N + tid];
+            if (nw.b != b && tid < N) parent = args().parent[(size_t)nw.b * N + tid];
             load_q(nw.b, nw.kvh);
-            if constexpr (kScored)
-                if (sc.slopes) slope = sc.slopes[nw.kvh * G + g] * sc.slope_mul;
+            if constexpr (kBiased) {
+                const auto& changed = late();
+                if (changed.slopes) slope = changed.slopes[nw.kvh * args().G + my_row().g] * changed.slope_mul;
+            }
         }
-        if (mt == 0 && tid == 0) work::note_parts(a, team, cw);
+        if (mt == 0 && tid == 0) work::note_parts(args(), team, cw);
     }
     // ---- write this lane's row: d = 32 db + 8 (j/4) + 4 g32 + (j%4)
     const int flagged = (work::tree_is_bad(a, spar) ? S4C_SEQ_BAD_TREE : 0) | (len_bad ? S4C_SEQ_BAD_LEN : 0);
-    if (a.status && tid == 0 && cw.tile == 0 && kvh == 0 && mt == 0) a.status[b] = flagged;
+    if (args().status && tid == 0 && cw.tile == 0 && kvh == 0 && mt == 0) args().status[b] = flagged;
     float l_tot = l_run + __shfl_xor(l_run, 32);
     if (flagged) {                             // zero output, whatever was read in place of a bad page
         l_tot = 0.f;
@@ -606,15 +646,17 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
             parts::put<kD, 1, MERGE, true>(Arguments().attn(), team, mt * WR + wave, 0, m_run, l_tot, [&](int q) __attribute__((always_inline)) {
                 return f32x4{o[q >> 2][4 * (q & 3)], o[q >> 2][4 * (q & 3) + 1], o[q >> 2][4 * (q & 3) + 2], o[q >> 2][4 * (q & 3) + 3]};
             });
-        }, score::writer(sc, kShift));
+        }, row_done);
         lens_end<STEP>(left);
         return;
     }
-    if (MERGE == parts::kWhole || work::walk_is_whole(a, cw)) {
+    if (MERGE == parts::kWhole || work::walk_is_whole(args(), cw)) {
         if (rvalid) {
-        if (g32 == 0) score::writer(sc, kShift)(((size_t)b * N + node) * a.Hq + kvh * G + g, m_run, l_tot);
+        const Row row = my_row();
+        const size_t at = ((size_t)b * args().N + row.node) * args().Hq + kvh * args().G + row.g;
+        if (row.half == 0) row_done(at, m_run, l_tot);
         const float inv = (l_tot > 0.f) ? 1.f / l_tot : 0.f;
-        bf16_t* orow = (bf16_t*)a.out + (((size_t)b * N + node) * a.Hq + kvh * G + g) * kD + 4 * g32;
+        bf16_t* orow = (bf16_t*)args().out + at * kD + 4 * row.half;
 #pragma unroll
         for (int db = 0; db < kDB; ++db)
 #pragma unroll
@@ -627,17 +669,18 @@ void tree_attn_mfma_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> s
         }
     } else {
         if (rvalid) {
-            const size_t prow = work::part_row(a, team, work::part_slot(cw)) + rq;
-            float* orow = Arguments().attn().ws_o + prow * kD + 4 * g32;       // (not kept in scratch while tiles are multiplied)
+            const Row row = my_row();
+            const size_t prow = work::part_row(args(), team, work::part_slot(cw)) + row.r;
+            float* orow = Arguments().attn().ws_o + prow * kD + 4 * row.half;       // (not kept in scratch while tiles are multiplied)
 #pragma unroll
             for (int db = 0; db < kDB; ++db)
 #pragma unroll
                 for (int jq = 0; jq < 4; ++jq)
                     *(float4*)(orow + 32 * db + 8 * jq) =
                         make_float4(o[db][4 * jq], o[db][4 * jq + 1], o[db][4 * jq + 2], o[db][4 * jq + 3]);
-            if (g32 == 0) {
-                a.ws_ml[prow * 2] = m_run;
-                a.ws_ml[prow * 2 + 1] = l_tot;
+            if (row.half == 0) {
+                args().ws_ml[prow * 2] = m_run;
+                args().ws_ml[prow * 2 + 1] = l_tot;
             }
         }
     }
@@ -651,14 +694,14 @@ int pick_wr(int M) { return M <= 128 ? 4 : 8; }
 
 template <int WR, int NS, int WPE, bool PAGED, bool F16, int D, StepKind STEP, parts::Merge MERGE, score::Kind SCORE = score::kPlain>
 hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st, const score::Args<SCORE>& sc = {}) {
-    constexpr int kLds = SCORE == score::kPlain ? lds_bytes_for(NS, D) : scored_lds_bytes_for(NS, D, WR);
+    constexpr int kLds = score::biased(SCORE) ? biased_lds_bytes_for(NS, D, WR) : lds_bytes_for(NS, D);
     static_assert((WR == 4 && D == 64 ? 2 : 1) * kLds <= 160 * 1024, "LDS of a CU");
     static std::atomic<uint64_t> lds_set{0};
     const hipError_t ea = ensure_dynamic_lds((const void*)tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE, SCORE>, kLds, lds_set);
     if (ea != hipSuccess) return ea;
     a.attn_wgs = attn_workgroups(a);
     const dim3 grid = launch_grid(a, rest_of(a, tail)), block(WR * 64);
-    hipLaunchKernelGGL((tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE, SCORE>), grid, block, kLds, st, a, tail, sc);
+    hipLaunchKernelGGL((tree_attn_mfma_kernel<WR, NS, WPE, PAGED, F16, D, STEP, MERGE, SCORE>), grid, block, kLds, st, score::with(a, sc), tail);
     return hipGetLastError();
 }
 

@@ -83,8 +83,9 @@ struct Cfg {
 
 template <class C, bool PAGED, StepKind STEP, parts::Merge MERGE, score::Kind SCORE>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kPerCu * C::kWaves / 4, 2)))
-void tree_attn_smallm_kernel(AttnArgs a, StepTail<STEP> tail, score::Args<SCORE> sc) {
+void tree_attn_smallm_kernel(score::Attn<SCORE> a, StepTail<STEP> tail) {
     constexpr bool kScored = SCORE != score::kPlain;
+    const auto& sc = score::of(a);
     constexpr int kD = C::kD, kKG = C::kKG, kRBW = C::kRBW, kNR = C::kNR, kRowB = C::kRowB;
     constexpr int kThreads = C::kThreads, kCH = C::kCH;
     constexpr bool kIs32 = C::kElem == kF32, F16 = C::kElem == kH16;
@@ -643,7 +644,7 @@ hipError_t launch(AttnArgs a, StepTail<STEP> tail, hipStream_t st, const score::
     if (ea != hipSuccess) return ea;
     a.attn_wgs = attn_workgroups(a);
     const dim3 grid = launch_grid(a, rest_of(a, tail)), block(C::kThreads);
-    hipLaunchKernelGGL((tree_attn_smallm_kernel<C, PAGED, STEP, MERGE, SCORE>), grid, block, kLds, st, a, tail, sc);
+    hipLaunchKernelGGL((tree_attn_smallm_kernel<C, PAGED, STEP, MERGE, SCORE>), grid, block, kLds, st, score::with(a, sc), tail);
     return hipGetLastError();
 }
 template <class C, bool PAGED, StepKind STEP>

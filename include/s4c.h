@@ -379,6 +379,8 @@ s4c_status s4c_tree_attn_scored_paged(const s4c_attn_shape* shape, const s4c_sco
  *              root_pos + k); root_pos is the root's of that attention call
  *   weight_in, weight  [B][Hkv][S_cap] fp32, the same array or two that do not overlap; rows from cache_len[b] on are not written
  *   status     [B] nullable: S4C_SEQ_BAD_LEN if cache_len, accept_len, the path or a page is not valid; nothing of that sequence is written.
+ * A sequence whose rows were not appended (flagged by s4c_kv_compact / s4c_commit_path: they did not fit) has no such rows, and its last
+ * ones would be taken for them: set its accept_len to -1, which is not valid here and adds nothing to root_pos.
  * S_cap <= 2^30.  Sums are fp32 in a fixed order: results are deterministic. */
 s4c_status s4c_kv_weigh(const s4c_attn_shape* shape, const s4c_score* score, const void* q, const void* k_cache, const float* lse,
                         const int32_t* cache_len, const int32_t* path, const int32_t* accept_len, int32_t max_path,

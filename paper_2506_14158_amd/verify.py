@@ -12,8 +12,9 @@ class TreeVerifier:
     """Pre-allocates outputs and workspaces for one shape and enqueues
     s4c_tree_attn -> s4c_accept_path -> s4c_kv_compact on the current stream.
 
-    For a cache that is kept to ``budget`` rows: step with a Score (its lse is kept), kv_weigh for every layer, root_pos advanced by
-    accept_len + 1, and kv_evict over all layers whenever the cache has grown far enough beyond the budget."""
+    For caches that are kept to ``budget`` rows: tree_attn_scored for every layer (each with an lse of its own), accept_path, commit_path over
+    all layers, kv_weigh for every layer, root_pos advanced by accept_len + 1, and kv_evict over all layers whenever the cache has grown far
+    enough beyond the budget.  A step with a Score is the attention, acceptance and compaction of a single layer, in three calls."""
 
     def __init__(self, B, N, Hq, Hkv, D, S_cap, V, dtype: torch.dtype, max_path: int, max_cache_len: int,
                  device="cuda", layers: int = 1, budget: int = 0, recent: int = 0):
@@ -60,7 +61,8 @@ class TreeVerifier:
 
     def kv_weigh(self, q, k_cache, cache_len, score: _b.Score, weight, scale: float = 0.0, lse=None):
         """After the path's rows were appended: what its rows attended to is added to ``weight`` [B][Hkv][S_cap], and their positions are
-        written into score.key_pos."""
+        written into score.key_pos.  Where they could not be appended (compact_status) there is nothing to weigh: an accept_len below 0
+        leaves a sequence as it is."""
         _b.s4c_kv_weigh(q, k_cache, self.lse if lse is None else lse, cache_len, self.path, self.accept_len, self.S_cap, score, weight, weight,
                         scale, self.weigh_status)
 

@@ -504,6 +504,13 @@ def _need(t, dtype, shape, what):
         raise TypeError("%s must be %s %s, got %s %s" % (what, dtype, list(shape), t.dtype, list(t.shape)))
 
 
+def _int32(x, what):
+    """ctypes would take the low bits of a larger number."""
+    if not -2 ** 31 <= int(x) < 2 ** 31:
+        raise ValueError("%s is beyond 32 bits: %s" % (what, x))
+    return int(x)
+
+
 def _one_device(*tensors):
     """The call goes to the current device's stream: its tensors have to be there."""
     here = torch.cuda.current_device()
@@ -557,11 +564,12 @@ def _tree_attn_scored(q, k_tree, v_tree, k_cache, v_cache, block_table, cache_le
         _need(lse, torch.float32, (B, N, Hq), "lse")
     if status is not None:
         _need(status, torch.int32, (B,), "status")
+    max_cache_len = _int32(max_cache_len, "max_cache_len")
     shape, sc = AttnShape(B, Hq, Hkv, D, N, S_cap, _dtype_code(q)), _score(score, B, Hq, Hkv, S_cap)
     _one_device(q, k_tree, v_tree, k_cache, v_cache, block_table, cache_len, parent, out, lse, status, workspace, *score[1:])
     entry = lib().s4c_tree_attn_scored_paged if pages else lib().s4c_tree_attn_scored
     _check(entry(C.byref(shape), C.byref(sc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), *pages, _ptr(cache_len),
-                 _ptr(parent), int(max_cache_len), float(scale), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), _bytes(workspace),
+                 _ptr(parent), max_cache_len, float(scale), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), _bytes(workspace),
                  _stream()))
     return out
 
@@ -608,11 +616,12 @@ def _kv_weigh(q, k_cache, block_table, lse, cache_len, path, accept_len, max_cac
         _need(t, torch.float32, (B, Hkv, S_cap), what)
     if status is not None:
         _need(status, torch.int32, (B,), "status")
+    max_cache_len = _int32(max_cache_len, "max_cache_len")
     shape, sc = AttnShape(B, Hq, Hkv, D, N, S_cap, _dtype_code(q)), _score(score, B, Hq, Hkv, S_cap)
     _one_device(q, k_cache, block_table, lse, cache_len, path, accept_len, weight_in, weight, status, *score[1:])
     entry = lib().s4c_kv_weigh_paged if pages else lib().s4c_kv_weigh
     _check(entry(C.byref(shape), C.byref(sc), _ptr(q), _ptr(k_cache), *pages, _ptr(lse), _ptr(cache_len), _ptr(path), _ptr(accept_len),
-                 int(path.shape[1]), int(max_cache_len), float(scale), _ptr(weight_in), _ptr(weight), _ptr(status), _stream()))
+                 int(path.shape[1]), max_cache_len, float(scale), _ptr(weight_in), _ptr(weight), _ptr(status), _stream()))
 
 
 def s4c_kv_weigh(q, k_cache, lse, cache_len, path, accept_len, max_cache_len: int, score: Score, weight_in, weight, scale: float = 0.0,
@@ -630,7 +639,8 @@ def s4c_kv_weigh_paged(q, k_pool, block_table, lse, cache_len, path, accept_len,
 
 
 def s4c_kv_evict_workspace_size(layers: int, B: int, Hkv: int, budget: int, S_cap: int) -> int:
-    return int(lib().s4c_kv_evict_workspace_size(layers, B, Hkv, budget, S_cap))
+    sizes = (_int32(x, "a size of the cache") for x in (layers, B, Hkv, budget, S_cap))
+    return int(lib().s4c_kv_evict_workspace_size(*sizes))
 
 
 def _kv_evict(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, budget, recent, weight, key_pos, new_len, workspace,
@@ -648,11 +658,12 @@ def _kv_evict(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, n
         _need(t, torch.int32, (B,), what)
     if kept is not None:
         _need(kept, torch.int32, (layers, B, Hkv, budget), "kept")
+    budget, recent = _int32(budget, "budget"), _int32(recent, "recent")
     shape = AttnShape(B, Hkv, Hkv, D, 1, S_cap, _dtype_code(k_cache))
     _one_device(k_cache, v_cache, block_table, weight_in, key_pos_in, cache_len, next_pos, weight, key_pos, new_len, workspace, kept, status)
     entry = lib().s4c_kv_evict_paged if pages else lib().s4c_kv_evict
     _check(entry(C.byref(shape), layers, _ptr(k_cache), _ptr(v_cache), *pages, _ptr(weight_in), _ptr(key_pos_in), _ptr(cache_len),
-                 _ptr(next_pos), int(budget), int(recent), _ptr(weight), _ptr(key_pos), _ptr(new_len), _ptr(kept), _ptr(status),
+                 _ptr(next_pos), budget, recent, _ptr(weight), _ptr(key_pos), _ptr(new_len), _ptr(kept), _ptr(status),
                  _ptr(workspace), _bytes(workspace), _stream()))
 
 

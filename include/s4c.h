@@ -344,8 +344,10 @@ typedef struct {
     const float* slopes;      /* [Hq] nullable: slopes[h] * (position of the key - position of the root) is added to it (a penalty on
                                  distance has slopes > 0).  For a node of depth d this differs from the distance to the node by
                                  slopes[h] * d on every key, which changes lse and not the output.  Without a cap, scale lies between
-                                 2^-60 and 2^60 then */
-    int32_t* key_pos;         /* [B][Hkv][S_cap] nullable: position of every cache row.  NULL: row j has position j, and the root
+                                 2^-60 and 2^60 then.  Products with distances (and scores, if there is no cap) stay below 2^23 in size: they
+                                 are fp32 numbers whose differences are exponents */
+    int32_t* key_pos;         /* [B][Hkv][S_cap] nullable: position of every cache row; its distance from the root is a 32-bit difference that
+                                 is taken as fp32, exact up to 2^24.  NULL: row j has position j, and the root
                                  the position of the row that it is appended to.  Read only where slopes are given; s4c_kv_weigh
                                  writes those of the path's rows */
     const int32_t* root_pos;  /* [B] position of node 0, required with key_pos; a node of depth d has root_pos + d */

@@ -71,3 +71,24 @@ def test_values_of_any_size(dtype, N, cap, bias):
     c.call(c.score(cap, bias))
     assert bool(torch.isfinite(c.out).all())
     c.check(c.score(cap, bias))
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("bias", ["rows", "kept"])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("dtype,N", [("bf16", 80), ("f16", 80), ("bf16", 7), ("f32", 20)])
+def test_a_bias_that_decides_alone(dtype, N, cap, bias, sign):
+    """Products with distances up to 2^22.6 (s4c.h: 2^23): a row's output is the value of its last key (its own), or of the first one.  Its exponential may be as far
+    from 1 as a product's rounding, and is rounded to the storage type, as the output is (half a step each)."""
+    c = Case(32, 2, N, 4, 2, 128, dtype, (300, 129), 320)
+    c.slopes = torch.full((4,), sign * 2.0 ** 14, device="cuda")
+    if bias == "kept":
+        c.pos = (1 << 30) + torch.arange(320, **I32).expand(2, 2, 320).contiguous()
+        c.root = (1 << 30) + c.len
+    c.call(c.score(cap, bias))
+    want = (c.vt if sign > 0 else c.vc[:, :, :1].transpose(1, 2).expand(2, N, 2, 128)).repeat_interleave(2, 2).double()
+    step = torch.finfo(DT[dtype]).eps / 2
+    assert bool(((c.out.double() - want).abs() <= 2.01 * step * want.abs()).all())
+    if sign > 0 and bias == "kept":
+        c.call(c.score(cap, "rows"))              # the same positions
+        assert bool(((c.out.double() - want).abs() <= 2.01 * step * want.abs()).all())

@@ -6,7 +6,7 @@ import pytest
 from tests.test_resources import resources
 
 MANY = ["tree_attn_mfma_%s_%s.hip" % (kind, t) for kind in ("lse", "slopes", "cap", "cap_slopes") for t in ("bf16", "f16")]
-FEW = ["tree_attn_smallm_scored_%s.hip" % t for t in ("bf16", "f16", "f32")]
+FEW = ["tree_attn_smallm_scored_bf16.hip"]             # (the one with most registers; a minute of compiling each)
 
 
 @pytest.fixture(scope="module")

@@ -63,7 +63,7 @@ void tree_attn_mfma_kernel(score::Attn<SCORE> a, StepTail<STEP> tail) {
     constexpr bool kCapped = SCORE == score::kCap || SCORE == score::kCapSlopes;
     const auto& sc = score::of(a);
     // (what a segment or a rare tile asks for is read then)
-    auto late = []() __attribute__((always_inline)) -> const auto& { return score::of(Arguments().attn<SCORE>()); };
+    auto late = []() __attribute__((always_inline)) -> decltype(auto) { return score::of(Arguments().attn<SCORE>()); };
     constexpr int NT = WR * 64;
     constexpr int BM = WR * 32;
     constexpr int kRowB = kD * 2;                // bytes per K/V row

@@ -20,6 +20,7 @@ SHARES = [
     Sizes("rows256-d64", "balanced", 7, 8, 4, 64, 47, "bf16", 8192, (2000, 63, 0, 1500, 640)),
     Sizes("rows128", "balanced", 7, 8, 4, 128, 20, "bf16", 8192, (1900, 5, 0, 1333, 64)),
     Sizes("rows128-d64", "balanced", 13, 8, 4, 64, 20, "f16", 8192, (1000, 0, 1, 64, 777, 8193)),
+    Sizes("rows128-70-sequences", "balanced", 70, 2, 4, 128, 20, "bf16", 3000, (300, 0, 64, 5, 400)),
     Sizes("rows64", "balanced", 3, 32, 1, 128, 37, "bf16", 24000, (2000, 0, 1111)),
     Sizes("rows32-d64", "balanced", 13, 16, 1, 64, 20, "f16", 3000, (32, 0, 1, 500, 3001)),
     Sizes("rows32-long", "balanced", 13, 16, 2, 64, 1, "bf16", 3000, (3000, 2901)),
